@@ -1,5 +1,6 @@
 /*
- * eaas.h -- C ABI of one stateless expert server's forward step on gfx950.
+ * eaas.h -- C ABI of one stateless expert server's forward step on gfx950, and of
+ * the separate products that train an expert layer or serve it in 8-bit integers.
  *
  * The operation (EaaS, §3.3 "Asynchronous Server Operation", and Fig. 5): the
  * server takes a batch of ready requests, reorganises the tokens by expert,
@@ -402,6 +403,128 @@ int eaas_expert_forward_noalloc(const eaas_shape *s, const void *x,
                                 const void *w_down, const float *w_down_scale,
                                 int w_dtype, void *out, int out_dtype,
                                 const eaas_routing *r, void *stream);
+
+/*
+ * The products of an expert layer on their own, for training the experts and
+ * for serving them in 8-bit integers.  eaas_expert_forward fuses them into one
+ * step; here each is a call, so that a caller can keep what a gradient needs.
+ *
+ * Rows are grouped by expert as by eaas_route_permute: group e holds the rows
+ * [offsets[e], offsets[e+1]), which may be none, and rows from offsets[E] on
+ * belong to no group: they are neither read into a result nor written.
+ *   offsets  [E+1] int32 (device), ascending from 0, at most R; values outside
+ *            are clamped to that range
+ * A row array has rows ld elements apart (ld >= its width): rows cut out of a
+ * wider array need no copy.  Its base needs no more alignment than an element;
+ * sizes, strides and bases that are multiples of 16 bytes are faster.  Weights
+ * W [E,N,K] are contiguous and 16-byte aligned.
+ *   perm, k  perm == NULL: row r of the product reads row r of x.  Otherwise x
+ *            is in token order, [R/k, K], R a multiple of k, and row r reads
+ *            token perm[r]/k (the perm of the routing, values clamped to
+ *            [0, R)): the reorganised copy of the tokens is never made.
+ * bf16 operands, products of them exact, sums in fp32; 8-bit operands, sums in
+ * int32.  Every sum is taken in a fixed order: equal calls give equal bits.
+ */
+typedef struct eaas_group_shape {
+  int32_t R; /* rows of the grouped arrays, >= 0                        */
+  int32_t E; /* groups, 1..1024                                         */
+  int32_t N; /* outputs of an expert's matrix (its rows), >= 1          */
+  int32_t K; /* inputs of an expert's matrix (its columns), >= 1        */
+} eaas_group_shape;
+
+/* Bytes of workspace that the four grouped products accept for this shape
+ * (partial sums, where a long sum is split over workgroups).  Conventions of
+ * `ws` as above.  0 for a shape the library rejects: see the limits at
+ * eaas_grouped_matmul. */
+size_t eaas_grouped_workspace_bytes(const eaas_group_shape *s);
+
+/* y[r,:] = W[e] x[src(r),:] for the rows r of every group e.
+ *   x [R or R/k, K] bf16 (ldx), w [E,N,K] bf16, y [R,N] bf16 or fp32 (ldy)
+ * y must not overlap x or w.  Errors: INVALID_ARG (null pointer, size below its
+ * least, ld below the width, k < 1 or R % k with perm, overlap, alignment),
+ * UNSUPPORTED (E > 1024, N*K or, with perm, (R/k)*ldx above 2^31 - 1, an ld
+ * above 2^22), WORKSPACE, HIP.  R = 0: nothing is enqueued. */
+int eaas_grouped_matmul(const eaas_group_shape *s, const void *x, int64_t ldx,
+                        const int32_t *perm, int32_t k, const int32_t *offsets,
+                        const void *w, void *y, int64_t ldy, int y_dtype,
+                        void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient in the rows: dx[r,:] = W[e]^T dy[r,:].
+ *   dy [R,N] bf16 (lddy), dx [R,K] bf16 or fp32 (lddx), in grouped order: with
+ * weights of 1, eaas_unpermute_combine sums fp32 dx into the tokens' gradients.
+ * Errors as eaas_grouped_matmul. */
+int eaas_grouped_matmul_dx(const eaas_group_shape *s, const void *dy, int64_t lddy,
+                           const int32_t *offsets, const void *w, void *dx, int64_t lddx,
+                           int dx_dtype, void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient in the weights: dW[e] = sum over the rows r of group e of
+ * dy[r,:] x[src(r),:]^T; zeros for a group without rows.
+ *   dw [E,N,K] bf16 or fp32, contiguous, 16-byte aligned
+ *   accumulate != 0 (fp32 only): dw += that sum (micro-batches of one step)
+ * R = 0 writes zeros (accumulate: nothing); dy, x and perm may then be NULL.
+ * Errors as eaas_grouped_matmul; INVALID_ARG for accumulate with bf16. */
+int eaas_grouped_matmul_dw(const eaas_group_shape *s, const void *dy, int64_t lddy,
+                           const void *x, int64_t ldx, const int32_t *perm, int32_t k,
+                           const int32_t *offsets, void *dw, int dw_dtype, int accumulate,
+                           void *ws, size_t ws_bytes, void *stream);
+
+/* Rows in 8-bit integers, one scale per row: s = amax/127 (1 for a row of
+ * zeros), q = x/s to the nearest integer, ties to even, in fp32 arithmetic with
+ * correctly rounded quotients.  A row that holds an infinity or a NaN gets a NaN
+ * scale and zero codes, so whatever is computed from it is NaN.
+ *   x [rows,K] bf16 (ldx), q [rows,K] int8 and s [rows] fp32, contiguous
+ * Quantizes activations per token, and weights [E,N,K] per output channel
+ * (rows = E*N).  rows = 0: nothing.  Errors: INVALID_ARG, UNSUPPORTED (rows or K
+ * above 2^31 - 1, K above 2^22), HIP. */
+int eaas_quantize_rows_int8(const void *x, int64_t ldx, int64_t rows, int32_t K, void *q,
+                            float *s, void *stream);
+
+/* The grouped product in 8-bit integers:
+ *   y[r,n] = (sum_k xq[src(r),k] wq[e,n,k]) * xs[src(r)] * wscale[e,n]
+ * with an exact int32 sum, rounded to fp32 before the two fp32 products (in this
+ * order).  xq [R or R/k, K] int8 contiguous with xs fp32 per row of xq, wq
+ * [E,N,K] int8, wscale [E,N] fp32, y [R,N] bf16 or fp32 (ldy).  K < 2^17 (the
+ * sum fits).  Errors as eaas_grouped_matmul. */
+int eaas_grouped_matmul_int8(const eaas_group_shape *s, const void *xq, const float *xs,
+                             const int32_t *perm, int32_t k, const int32_t *offsets,
+                             const void *wq, const float *wscale, void *y, int64_t ldy,
+                             int y_dtype, void *ws, size_t ws_bytes, void *stream);
+
+/* The activation between the products, for rows of the grouped arrays:
+ *   h = silu(gate) * up,  silu(g) = g / (1 + exp(-g)), in fp32
+ *   gu      [rows,2I] bf16, contiguous: gate columns [0,I), up columns [I,2I)
+ *   h       [rows,I] bf16 (rounded once), contiguous
+ *   n_rows  NULL, or a device int32 (offsets + E of the routing): only the first
+ *           min(rows, max(0, *n_rows)) rows are read and written
+ * rows = 0: nothing.  Errors: INVALID_ARG (null, overlap of an output with an
+ * input, element alignment), UNSUPPORTED (rows or I above 2^31 - 1, I above
+ * 2^21), HIP. */
+int eaas_swiglu(const void *gu, int64_t rows, int32_t I, const int32_t *n_rows, void *h,
+                void *stream);
+
+/* The same, quantized as by eaas_quantize_rows_int8 instead of rounded to bf16
+ * (codes and scales are those of the fp32 h): q [rows,I] int8, s [rows] fp32. */
+int eaas_swiglu_int8(const void *gu, int64_t rows, int32_t I, const int32_t *n_rows, void *q,
+                     float *s, void *stream);
+
+/* Its gradient: with t = 1 / (1 + exp(-gate)),
+ *   dgate = dh up t (1 + gate (1 - t)),  dup = dh gate t
+ *   dh [rows,I] bf16, dgu [rows,2I] bf16 (dgate, then dup), contiguous.  dgu may
+ *   be gu itself (exactly); no other overlap. */
+int eaas_swiglu_backward(const void *gu, const void *dh, int64_t rows, int32_t I,
+                         const int32_t *n_rows, void *dgu, void *stream);
+
+/* Gradients of eaas_unpermute_combine: for every valid slot t*k+j at row r,
+ *   dy_perm[r,:]      = topk_weights[t,j] * dout[t,:]        (bf16)
+ *   dweights[t,j]     = sum over c of dout[t,c] * y_perm[r,c]   (fp32)
+ * dweights of an invalid slot is 0; rows of dy_perm past the valid ones are left
+ * untouched.
+ *   dout [T,H] bf16 or fp32, y_perm [R,H] fp32, dy_perm [R,H] bf16, dweights
+ *   [T,k] fp32; outputs overlap nothing.  Errors as eaas_unpermute_combine. */
+int eaas_unpermute_combine_backward(const eaas_shape *s, const void *dout, int dout_dtype,
+                                    const float *y_perm, const eaas_routing *r,
+                                    const float *topk_weights, void *dy_perm, float *dweights,
+                                    void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *eaas_status_string(int status);

@@ -1,0 +1,393 @@
+// Grouped products of an expert's matrix, for any size, stride and alignment:
+// forward, gradient in the rows, gradient in the weights, and the forward in
+// 8-bit integers (grouped.h states the three products in one frame).
+//
+// A workgroup of four waves computes a tile of 128 x 128 results; a wave holds
+// 64 x 64 of them as 2 x 2 blocks of v_mfma_f32_32x32x16_bf16 (8-bit integers:
+// v_mfma_i32_32x32x32_i8).  Tiles of both operands, 16 KiB each, pass through
+// registers into one of two LDS stages while the other is multiplied: loads into
+// registers take any byte alignment, and what lies past an edge is replaced by
+// zeros there.  An operand that lies along the sum is kept as rows of 128 bytes
+// and read back 16 bytes a lane; one that lies across it is kept as it comes, 64
+// rows of 128 columns, and read with the transposing LDS load, which hands each
+// lane four elements of its column.
+#include <algorithm>
+
+#include "grouped.h"
+
+namespace eaas {
+namespace {
+
+constexpr int kBI = 128, kBJ = 128, kThreads = 256;
+constexpr int kStage = 16384;  // bytes of one operand's tile
+
+__device__ __forceinline__ int swz_along(int row) { return (row & 7) ^ ((row >> 3) & 1); }
+// the transposing load's 16 lanes take 4 rows x 32 bytes: neighbouring rows go
+// to different quarters of the 256 bytes that all banks span
+__device__ __forceinline__ int swz_across(int row) { return (row & 3) << 2; }
+
+// 16 bytes at an address of element alignment.
+__device__ __forceinline__ u32x4 load16(const char* p) {
+  u32x4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+
+// The first n elements of 16 bytes, zeros after them.
+template <int ESZ>
+__device__ __forceinline__ u32x4 load_some(const char* p, int n) {
+  u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+  for (int c = 0; c < 16 / ESZ; ++c) {
+    if (c >= n) break;
+    const uint32_t b = ESZ == 2 ? *reinterpret_cast<const uint16_t*>(p + 2 * c)
+                                : *reinterpret_cast<const uint8_t*>(p + c);
+    const int at = c * ESZ;
+    v[at / 4] |= b << (8 * (at % 4));
+  }
+  return v;
+}
+
+// One operand's tile on its way from memory to LDS.
+//   ACROSS: rows are the sum's index [s0, s0 + 64) up to s_end, columns
+//           [c0, c0 + 128) of `width`
+//   else:   128 rows (pointers fixed for the whole sum), 128 bytes of the sum
+template <bool ACROSS, int ESZ>
+struct Loader {
+  static constexpr int EPC = 16 / ESZ;  // elements of a chunk
+  const char* row[4];                   // along: this thread's rows
+  int chunk, r0;
+  u32x4 v[4];
+
+  template <class RowPtr>
+  __device__ __forceinline__ void init(RowPtr rp) {
+    const int tid = threadIdx.x;
+    if constexpr (ACROSS) {
+      chunk = tid & 15;
+      r0 = tid >> 4;
+    } else {
+      chunk = tid & 7;
+      r0 = tid >> 3;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) row[q] = rp(r0 + 32 * q);
+    }
+  }
+  // s0: the sum's index where the tile starts; s_end: where the sum ends
+  template <class RowPtr>
+  __device__ __forceinline__ void load(RowPtr rp, int s0, int s_end, int c0, int width) {
+    if constexpr (ACROSS) {
+      const int c = c0 + chunk * EPC;
+      const bool inside = s0 + 64 <= s_end && c0 + 128 <= width;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int s = s0 + r0 + 16 * q;
+        if (inside) {
+          v[q] = load16(rp(s) + (size_t)c * ESZ);
+        } else {
+          v[q] = u32x4{0, 0, 0, 0};
+          if (s < s_end && c < width) {
+            const char* p = rp(s) + (size_t)c * ESZ;
+            v[q] = c + EPC <= width ? load16(p) : load_some<ESZ>(p, width - c);
+          }
+        }
+      }
+    } else {
+      const int s = s0 + chunk * EPC;
+      const bool inside = s0 + 8 * EPC <= s_end;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const char* p = row[q] + (size_t)s * ESZ;
+        if (inside) {
+          v[q] = load16(p);
+        } else {
+          v[q] = u32x4{0, 0, 0, 0};
+          if (s < s_end) v[q] = s + EPC <= s_end ? load16(p) : load_some<ESZ>(p, s_end - s);
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void store(LDS_AS char* stage) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if constexpr (ACROSS) {
+        const int r = r0 + 16 * q;
+        *reinterpret_cast<LDS_AS u32x4*>(stage + r * 256 + ((chunk ^ swz_across(r)) << 4)) = v[q];
+      } else {
+        const int r = r0 + 32 * q;
+        *reinterpret_cast<LDS_AS u32x4*>(stage + r * 128 + ((chunk ^ swz_along(r)) << 4)) = v[q];
+      }
+    }
+  }
+};
+
+// Fragment of k-step kk for the 32 rows (along) or columns (across) from c0: lane
+// l holds element l % 32 and 16 bytes of the sum, the half l / 32 of the step.
+template <bool ACROSS>
+__device__ __forceinline__ u32x4 fragment(const LDS_AS char* stage, int c0, int kk) {
+  const int lane = threadIdx.x & (kWave - 1);
+  if constexpr (ACROSS) {
+    const int g = lane >> 4, i = lane & 15;
+    const int c = c0 + (g & 1) * 16 + (i & 3) * 4;
+    u32x4 f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int s = kk * 16 + (g >> 1) * 8 + h * 4 + (i >> 2);
+      const LDS_AS char* at = stage + s * 256 + (((c >> 3) ^ swz_across(s)) << 4) + (c & 7) * 2;
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)at);
+      const u32x2 w = __builtin_bit_cast(u32x2, t);
+      f[2 * h] = w[0];
+      f[2 * h + 1] = w[1];
+    }
+    return f;
+  } else {
+    const int r = c0 + (lane & 31);
+    return *reinterpret_cast<const LDS_AS u32x4*>(stage + r * 128 +
+                                                  (((2 * kk + (lane >> 5)) ^ swz_along(r)) << 4));
+  }
+}
+
+template <int DIR, bool I8>
+__global__ __launch_bounds__(kThreads) void grouped_any_kernel(GroupedParams p) {
+  constexpr bool A_ACROSS = DIR == kGradWeights, B_ACROSS = DIR != kForward;
+  constexpr int ESZ = I8 ? 1 : 2;
+  constexpr int SUM = 128 / ESZ;  // the sum's elements in a tile
+  static_assert(!I8 || DIR == kForward, "8-bit integers: forward only");
+  __shared__ __attribute__((aligned(16))) char smem[4 * kStage];
+  __shared__ int s_find[kThreads / kWave + 4];
+  GroupedTile t;
+  if (!find_tile<DIR, kBI, kBJ, kThreads>(p, s_find, t)) return;
+
+  const int cols = columns<DIR>(p);
+  const int sum_end = DIR == kForward ? p.K : DIR == kGradRows ? p.N : t.end - t.beg;
+  const int tiles = ceil_div(sum_end, SUM);
+  const int split = blockIdx.y;
+  const int first = (int)((long long)tiles * split / p.splits);
+  const int last = (int)((long long)tiles * (split + 1) / p.splits);
+
+  const char* w = p.b + (DIR == kGradWeights ? 0 : (size_t)t.e * p.N * p.K * ESZ);
+  // rows past the tile's repeat one that exists; their results are not stored
+  auto a_row = [&](int i) {
+    if (DIR == kGradWeights) return p.a + (size_t)(t.beg + i) * p.lda * ESZ;
+    const int r = t.i0 + min(i, t.i_valid - 1);
+    return p.a + (size_t)(DIR == kForward ? source_row(p, r) : r) * p.lda * ESZ;
+  };
+  auto b_row = [&](int j) {
+    if (DIR == kForward) return w + (size_t)min(t.j0 + j, cols - 1) * p.ldb * ESZ;
+    if (DIR == kGradRows) return w + (size_t)j * p.ldb * ESZ;
+    return w + (size_t)source_row(p, t.beg + j) * p.ldb * ESZ;
+  };
+  Loader<A_ACROSS, ESZ> la;
+  Loader<B_ACROSS, ESZ> lb;
+  la.init(a_row);
+  lb.init(b_row);
+  auto load = [&](int kt) {
+    la.load(a_row, kt * SUM, sum_end, t.i0, p.N);
+    lb.load(b_row, kt * SUM, sum_end, t.j0, cols);
+  };
+
+  typedef typename std::conditional<I8, i32x16, f32x16>::type Acc;
+  Acc acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = Acc{};
+  const int wave = threadIdx.x / kWave;
+  const int wi = (wave & 1) * 64, wj = (wave >> 1) * 64;
+  LDS_AS char* lds = (LDS_AS char*)smem;
+
+  if (first < last) {
+    load(first);
+    la.store(lds);
+    lb.store(lds + kStage);
+    __syncthreads();
+    for (int kt = first; kt < last; ++kt) {
+      const int cur = (kt - first) & 1;
+      if (kt + 1 < last) load(kt + 1);
+      const LDS_AS char* sa = lds + cur * 2 * kStage;
+      const LDS_AS char* sb = sa + kStage;
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) {
+        u32x4 fa[2], fb[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fa[i] = fragment<A_ACROSS>(sa, wi + 32 * i, kk);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) fb[j] = fragment<B_ACROSS>(sb, wj + 32 * j, kk);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            if constexpr (I8)
+              acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(
+                  __builtin_bit_cast(i32x4, fb[j]), __builtin_bit_cast(i32x4, fa[i]), acc[i][j], 0,
+                  0, 0);
+            else
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                  __builtin_bit_cast(bf16x8, fb[j]), __builtin_bit_cast(bf16x8, fa[i]), acc[i][j],
+                  0, 0, 0);
+          }
+      }
+      if (kt + 1 < last) {
+        la.store(lds + (cur ^ 1) * 2 * kStage);
+        lb.store(lds + (cur ^ 1) * 2 * kStage + kStage);
+      }
+      __syncthreads();
+    }
+  }
+
+  // acc[i][j][v]: row i*32 + lane % 32, column j*32 + 8*(v/4) + 4*(lane/32) + v % 4
+  const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int ri = wi + 32 * i + (lane & 31);
+    if (ri >= t.i_valid) continue;
+    const int row = t.i0 + ri;
+    float rs = 0.0f;
+    if constexpr (I8) rs = p.row_scale[source_row(p, row)];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = t.j0 + wj + 32 * j + 8 * q + 4 * (lane >> 5);
+        if (col >= cols) continue;
+        if (p.splits > 1) {
+          const size_t at = part_at<DIR>(p, split, t.e, row, col);
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (col + c < cols) {
+              if constexpr (I8) static_cast<int*>(p.part)[at + c] = acc[i][j][4 * q + c];
+              else static_cast<float*>(p.part)[at + c] = acc[i][j][4 * q + c];
+            }
+          continue;
+        }
+        if constexpr (I8) {
+          i32x4 v;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[c] = acc[i][j][4 * q + c];
+          store4<DIR>(p, t.e, row, col, scaled(p, t.e, rs, col, v));
+        } else {
+          f32x4 v;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) v[c] = acc[i][j][4 * q + c];
+          store4<DIR>(p, t.e, row, col, v);
+        }
+      }
+  }
+}
+
+// The parts of a split sum joined, in ascending order: one thread for four
+// columns of one row.
+template <int DIR, bool I8>
+__global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p) {
+  const int cols = columns<DIR>(p);
+  const int quads = ceil_div(cols, 4);
+  const long long rows = DIR == kGradWeights ? (long long)p.E * p.N
+                                             : min(max(p.offsets[p.E], 0), p.R);
+  const long long first = DIR == kGradWeights ? 0 : min(max(p.offsets[0], 0), p.R);
+  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (rows - first) * quads;
+       u += (long long)gridDim.x * 256) {
+    const long long row = first + u / quads;
+    const int j = (int)(u % quads) * 4;
+    const int e = DIR == kGradWeights ? (int)(row / p.N) : 0;
+    const int i = DIR == kGradWeights ? (int)(row % p.N) : (int)row;
+    if constexpr (I8) {
+      i32x4 v = {0, 0, 0, 0};
+      for (int s = 0; s < p.splits; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (j + c < cols) v[c] += static_cast<const int*>(p.part)[part_at<DIR>(p, s, e, i, j + c)];
+      // the group whose rows hold i: the last that starts at or before it and is not empty
+      int lo = 0, hi = p.E - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.offsets[mid] <= i) lo = mid; else hi = mid - 1;
+      }
+      store4<DIR>(p, lo, i, j, scaled(p, lo, p.row_scale[source_row(p, i)], j, v));
+    } else {
+      f32x4 v = {0, 0, 0, 0};
+      for (int s = 0; s < p.splits; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (j + c < cols)
+            v[c] += static_cast<const float*>(p.part)[part_at<DIR>(p, s, e, i, j + c)];
+      store4<DIR>(p, e, i, j, v);
+    }
+  }
+}
+
+// Row tiles of all groups together, at most: every group may end in a part tile.
+long long most_row_tiles(const GroupedArgs& a, int bi) {
+  return a.R / bi + std::min(a.R, a.E);
+}
+
+long long out_tiles(const GroupedArgs& a, int bi, int bj) {
+  if (a.dir == kForward) return most_row_tiles(a, bi) * ceil_div(a.N, bj);
+  if (a.dir == kGradRows) return most_row_tiles(a, bi) * ceil_div(a.K, bj);
+  return (long long)a.E * ceil_div(a.N, bi) * ceil_div(a.K, bj);
+}
+
+// Parts of the sum: where the tiles alone leave most of the 256 CUs idle, as
+// many as give two workgroups to a CU, of at least 8 tiles of the sum each.
+int sum_parts(const GroupedArgs& a) {
+  const long long tiles = out_tiles(a, kBI, kBJ);
+  const int sum = a.dir == kForward ? a.K : a.dir == kGradRows ? a.N : a.R;
+  const int steps = ceil_div(sum, a.i8 ? 128 : 64);
+  if (tiles >= 192 || steps < 16) return 1;
+  return (int)std::max<long long>(1, std::min<long long>(512 / tiles, steps / 8));
+}
+
+template <int DIR, bool I8>
+hipError_t launch_any(GroupedParams p, const GroupedArgs& a, hipStream_t stream) {
+  const long long tiles = out_tiles(a, kBI, kBJ);
+  if (tiles <= 0) return hipSuccess;
+  if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
+  p.splits = sum_parts(a);
+  hipLaunchKernelGGL((grouped_any_kernel<DIR, I8>), dim3((unsigned)tiles, (unsigned)p.splits),
+                     dim3(kThreads), 0, stream, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const long long rows = DIR == kGradWeights ? (long long)a.E * a.N : a.R;
+  const long long quads = rows * ceil_div(DIR == kForward ? a.N : a.K, 4);
+  hipLaunchKernelGGL((grouped_join_kernel<DIR, I8>),
+                     dim3((unsigned)std::min<long long>((quads + 255) / 256, 4096)), dim3(256), 0,
+                     stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t grouped_workspace(const GroupedArgs& a) {
+  const int parts = sum_parts(a);
+  if (parts == 1) return 0;
+  const size_t rows = a.dir == kGradWeights ? (size_t)a.E * a.N : (size_t)a.R;
+  return (size_t)parts * rows * (a.dir == kForward ? a.N : a.K) * 4;
+}
+
+hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream) {
+  GroupedParams p{};
+  p.a = static_cast<const char*>(a.a);
+  p.lda = a.lda;
+  p.b = static_cast<const char*>(a.b);
+  p.ldb = a.dir == kGradWeights ? a.ldb : a.K;
+  p.perm = a.perm;
+  p.k = a.k;
+  p.offsets = a.offsets;
+  p.R = a.R;
+  p.E = a.E;
+  p.N = a.N;
+  p.K = a.K;
+  p.out = a.out;
+  p.ldo = a.ldo;
+  p.out_fp32 = a.out_fp32;
+  p.accumulate = a.accumulate;
+  p.vec = a.ldo % 4 == 0 && (uintptr_t)a.out % (a.out_fp32 ? 16 : 8) == 0;
+  p.row_scale = a.row_scale;
+  p.col_scale = a.col_scale;
+  p.part = a.ws;
+  if (a.i8) return launch_any<kForward, true>(p, a, stream);
+  if (a.dir == kForward) return launch_any<kForward, false>(p, a, stream);
+  if (a.dir == kGradRows) return launch_any<kGradRows, false>(p, a, stream);
+  return launch_any<kGradWeights, false>(p, a, stream);
+}
+
+}  // namespace eaas

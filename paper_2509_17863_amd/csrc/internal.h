@@ -145,4 +145,40 @@ hipError_t launch_slot_snapshot(const eaas_slot* slots, int n_slots, int cap, in
 hipError_t launch_slot_complete(const eaas_slot* slots, int n_slots, const int32_t* taken,
                                 hipStream_t stream);
 
+// Grouped products of an expert's matrix on their own (grouped.h has the frame).
+enum GroupedDir { kForward = 0, kGradRows = 1, kGradWeights = 2 };
+struct GroupedArgs {
+  int dir;                  // GroupedDir
+  bool i8;                  // 8-bit integers (forward)
+  int R, E, N, K;
+  const void* a;            // x | dy | dy, lda elements between rows
+  long long lda;
+  const void* b;            // W | W | x (ldb)
+  long long ldb;
+  const int32_t* perm;      // of x's rows; nullptr: in place
+  int k;
+  const int32_t* offsets;
+  void* out;
+  long long ldo;
+  bool out_fp32, accumulate;
+  const float* row_scale;   // 8-bit integers
+  const float* col_scale;
+  void* ws;                 // grouped_workspace bytes
+};
+size_t grouped_workspace(const GroupedArgs& a);  // (a's sizes only)
+hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream);
+
+// Activation, 8-bit rows and the combine's gradient (activation.hip).
+hipError_t launch_swiglu(const uint16_t* gu, long long rows, int I, const int32_t* n_rows,
+                         uint16_t* h, hipStream_t stream);
+hipError_t launch_swiglu_backward(const uint16_t* gu, const uint16_t* dh, long long rows, int I,
+                                  const int32_t* n_rows, uint16_t* dgu, hipStream_t stream);
+hipError_t launch_quantize_int8(const uint16_t* x, long long ldx, long long rows, int K, int8_t* q,
+                                float* s, hipStream_t stream);
+hipError_t launch_swiglu_int8(const uint16_t* gu, long long rows, int I, const int32_t* n_rows,
+                              int8_t* q, float* s, hipStream_t stream);
+hipError_t launch_combine_backward(const void* dout, bool dout_fp32, const float* y,
+                                   const int32_t* inv, const float* w, int T, int H, int k,
+                                   uint16_t* dy, float* dw, hipStream_t stream);
+
 }  // namespace eaas

@@ -25,6 +25,10 @@ __all__ = [
     "eaas_workspace_bytes_for", "EAAS_ENTRY_ROUTE_PERMUTE", "EAAS_ENTRY_FFN_GROUPED",
     "EAAS_ENTRY_FORWARD", "eaas_expert_forward_noalloc", "EAAS_NOALLOC_SCRATCH_BYTES",
     "use_library", "EAAS_FP8_E4M3_TILED", "EAAS_GATE_UP", "EAAS_DOWN", "eaas_tile_weights_fp8",
+    "eaas_grouped_workspace_bytes", "alloc_grouped_workspace", "eaas_grouped_matmul",
+    "eaas_grouped_matmul_dx", "eaas_grouped_matmul_dw", "eaas_quantize_rows_int8",
+    "eaas_grouped_matmul_int8", "eaas_swiglu", "eaas_swiglu_int8", "eaas_swiglu_backward",
+    "eaas_unpermute_combine_backward",
 ]
 
 EAAS_OK = 0
@@ -39,7 +43,11 @@ EXPORTED = ("eaas_workspace_bytes", "eaas_route_permute", "eaas_expert_ffn_group
             "eaas_status_string", "eaas_segments_workspace_bytes",
             "eaas_expert_forward_segments", "eaas_server_workspace_bytes", "eaas_server_step",
             "eaas_quantize_rows_fp8", "eaas_workspace_region", "eaas_workspace_bytes_for",
-            "eaas_expert_forward_noalloc", "eaas_tile_weights_fp8")
+            "eaas_expert_forward_noalloc", "eaas_tile_weights_fp8",
+            "eaas_grouped_workspace_bytes", "eaas_grouped_matmul", "eaas_grouped_matmul_dx",
+            "eaas_grouped_matmul_dw", "eaas_quantize_rows_int8", "eaas_grouped_matmul_int8",
+            "eaas_swiglu", "eaas_swiglu_int8", "eaas_swiglu_backward",
+            "eaas_unpermute_combine_backward")
 
 _DEFAULT_LIB = Path(__file__).resolve().parent / "libeaas.so"
 _LIB_PATH = _DEFAULT_LIB
@@ -55,6 +63,11 @@ class EaasError(RuntimeError):
 class _Shape(ctypes.Structure):
     _fields_ = [("T", ctypes.c_int32), ("H", ctypes.c_int32), ("I", ctypes.c_int32),
                 ("E", ctypes.c_int32), ("k", ctypes.c_int32)]
+
+
+class _GroupShape(ctypes.Structure):
+    _fields_ = [("R", ctypes.c_int32), ("E", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("K", ctypes.c_int32)]
 
 
 class _Routing(ctypes.Structure):
@@ -105,6 +118,25 @@ def _bind(L: ctypes.CDLL) -> ctypes.CDLL:
     L.eaas_workspace_region.restype = i32
     L.eaas_internal_gemm_plan.argtypes = [sp, i32, i32, i32, vp]
     L.eaas_internal_gemm_plan.restype = i32
+    gp, i64 = ctypes.POINTER(_GroupShape), ctypes.c_int64
+    L.eaas_grouped_workspace_bytes.argtypes = [gp]
+    L.eaas_grouped_workspace_bytes.restype = sz
+    L.eaas_grouped_matmul.argtypes = [gp, vp, i64, vp, ctypes.c_int32, vp, vp, vp, i64, i32, vp,
+                                      sz, vp]
+    L.eaas_grouped_matmul_dx.argtypes = [gp, vp, i64, vp, vp, vp, i64, i32, vp, sz, vp]
+    L.eaas_grouped_matmul_dw.argtypes = [gp, vp, i64, vp, i64, vp, ctypes.c_int32, vp, vp, i32,
+                                         i32, vp, sz, vp]
+    L.eaas_grouped_matmul_int8.argtypes = [gp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, i64,
+                                           i32, vp, sz, vp]
+    L.eaas_quantize_rows_int8.argtypes = [vp, i64, i64, ctypes.c_int32, vp, vp, vp]
+    L.eaas_swiglu.argtypes = [vp, i64, ctypes.c_int32, vp, vp, vp]
+    L.eaas_swiglu_int8.argtypes = [vp, i64, ctypes.c_int32, vp, vp, vp, vp]
+    L.eaas_swiglu_backward.argtypes = [vp, vp, i64, ctypes.c_int32, vp, vp, vp]
+    L.eaas_unpermute_combine_backward.argtypes = [sp, vp, i32, vp, rp, vp, vp, vp, vp]
+    for name in ("eaas_grouped_matmul", "eaas_grouped_matmul_dx", "eaas_grouped_matmul_dw",
+                 "eaas_grouped_matmul_int8", "eaas_quantize_rows_int8", "eaas_swiglu",
+                 "eaas_swiglu_int8", "eaas_swiglu_backward", "eaas_unpermute_combine_backward"):
+        getattr(L, name).restype = i32
     L.eaas_status_string.argtypes = [i32]
     L.eaas_status_string.restype = ctypes.c_char_p
     return L
@@ -430,3 +462,196 @@ def eaas_server_step(slots: torch.Tensor, n_slots: int, layers: torch.Tensor, n_
     st = lib().eaas_server_step(ctypes.byref(s), _p(slots), int(n_slots), _p(layers),
                                 int(n_layers), int(w_dtype), _p(ws), ws.numel(), _stream(stream))
     _check(st, "eaas_server_step")
+
+
+# ------------------------------------------------------------ separate products
+def _rows(t: torch.Tensor, width: int, dtype=None) -> tuple[int, int]:
+    """(pointer, elements between rows) of a 2-D tensor with dense rows."""
+    if t.dim() != 2 or t.shape[1] != width:
+        raise ValueError(f"expected rows of {width} elements, got {tuple(t.shape)}")
+    if dtype is not None and t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+        raise ValueError(f"expected {dtype}, got {t.dtype}")
+    if width > 1 and t.stride(1) != 1:
+        raise ValueError("the elements of a row must be adjacent")
+    # (one row, or none, may carry any stride)
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+
+
+_OUT = {torch.bfloat16: EAAS_BF16, torch.float32: EAAS_FP32}
+
+
+def _dense(t: torch.Tensor, dtype, *shape) -> int:
+    if t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    return _p(t)
+
+
+def _group_shape(R, E, N, K) -> _GroupShape:
+    return _GroupShape(int(R), int(E), int(N), int(K))
+
+
+def _gather(x: torch.Tensor, R: int, perm, k: int) -> tuple[int | None, int]:
+    """(perm's pointer, k), after checking the rows of x."""
+    if perm is None:
+        if x.shape[0] != R:
+            raise ValueError(f"x has {x.shape[0]} rows, expected {R}")
+        return None, 1
+    if x.shape[0] * k != R:
+        raise ValueError(f"x has {x.shape[0]} tokens of {k} slots, expected {R} rows in all")
+    return _dense(perm, torch.int32, R), int(k)
+
+
+def eaas_grouped_workspace_bytes(R, E, N, K) -> int:
+    return int(lib().eaas_grouped_workspace_bytes(ctypes.byref(_group_shape(R, E, N, K))))
+
+
+def alloc_grouped_workspace(R, E, N, K, device="cuda") -> torch.Tensor:
+    """Workspace of the grouped products of R rows with E matrices [N, K]."""
+    n = eaas_grouped_workspace_bytes(R, E, N, K)
+    if n == 0:
+        raise EaasError(-2, "eaas_grouped_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def eaas_grouped_matmul(x: torch.Tensor, offsets: torch.Tensor, w: torch.Tensor, y: torch.Tensor,
+                        ws: torch.Tensor, perm=None, k: int = 1, stream=None) -> None:
+    """y[r] = w[e] @ x[r] for the rows r of each group e, [offsets[e],
+    offsets[e+1]).  x [R, K] bf16, or, with the routing's perm, the tokens
+    [R/k, K]; w [E, N, K] bf16; y [R, N] bf16 or fp32.  Rows of x and y may be
+    cut out of wider arrays."""
+    E, N, K = w.shape
+    R = y.shape[0]
+    xp, ldx = _rows(x, K, torch.bfloat16)
+    yp, ldy = _rows(y, N, (torch.bfloat16, torch.float32))
+    pp, kk = _gather(x, R, perm, k)
+    s = _group_shape(R, E, N, K)
+    _check(lib().eaas_grouped_matmul(
+        ctypes.byref(s), xp, ldx, pp, kk, _dense(offsets, torch.int32, E + 1),
+        _dense(w, torch.bfloat16, E, N, K), yp, ldy, _OUT[y.dtype], _p(ws), ws.numel(),
+        _stream(stream)), "eaas_grouped_matmul")
+
+
+def eaas_grouped_matmul_dx(dy: torch.Tensor, offsets: torch.Tensor, w: torch.Tensor,
+                           dx: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """dx[r] = w[e]^T @ dy[r]: dy [R, N] bf16, dx [R, K] bf16 or fp32."""
+    E, N, K = w.shape
+    R = dx.shape[0]
+    if dy.shape[0] != R:
+        raise ValueError(f"dy has {dy.shape[0]} rows, dx {R}")
+    dyp, lddy = _rows(dy, N, torch.bfloat16)
+    dxp, lddx = _rows(dx, K, (torch.bfloat16, torch.float32))
+    s = _group_shape(R, E, N, K)
+    _check(lib().eaas_grouped_matmul_dx(
+        ctypes.byref(s), dyp, lddy, _dense(offsets, torch.int32, E + 1),
+        _dense(w, torch.bfloat16, E, N, K), dxp, lddx, _OUT[dx.dtype], _p(ws), ws.numel(),
+        _stream(stream)), "eaas_grouped_matmul_dx")
+
+
+def eaas_grouped_matmul_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor,
+                           dw: torch.Tensor, ws: torch.Tensor, perm=None, k: int = 1,
+                           accumulate: bool = False, stream=None) -> None:
+    """dw[e] = sum over the group's rows of outer(dy[r], x[r]) (accumulate: added
+    to an fp32 dw).  dy [R, N] bf16, x as in eaas_grouped_matmul, dw [E, N, K]
+    bf16 or fp32."""
+    E, N, K = dw.shape
+    R = dy.shape[0]
+    dyp, lddy = _rows(dy, N, torch.bfloat16)
+    xp, ldx = _rows(x, K, torch.bfloat16)
+    pp, kk = _gather(x, R, perm, k)
+    if dw.dtype not in _OUT:
+        raise ValueError(f"dw must be bf16 or fp32, got {dw.dtype}")
+    s = _group_shape(R, E, N, K)
+    _check(lib().eaas_grouped_matmul_dw(
+        ctypes.byref(s), dyp, lddy, xp, ldx, pp, kk, _dense(offsets, torch.int32, E + 1), _p(dw),
+        _OUT[dw.dtype], int(accumulate), _p(ws), ws.numel(), _stream(stream)),
+        "eaas_grouped_matmul_dw")
+
+
+def eaas_quantize_rows_int8(x: torch.Tensor, q: torch.Tensor, s: torch.Tensor,
+                            stream=None) -> None:
+    """x [rows, K] bf16 -> q [rows, K] int8 and s [rows] fp32 (s = amax / 127).
+    Weights [E, N, K] are quantized per output channel as E*N rows."""
+    rows, K = x.shape
+    xp, ldx = _rows(x, K, torch.bfloat16)
+    _check(lib().eaas_quantize_rows_int8(xp, ldx, rows, K, _dense(q, torch.int8, rows, K),
+                                         _dense(s, torch.float32, rows), _stream(stream)),
+           "eaas_quantize_rows_int8")
+
+
+def eaas_grouped_matmul_int8(xq: torch.Tensor, xs: torch.Tensor, offsets: torch.Tensor,
+                             wq: torch.Tensor, wscale: torch.Tensor, y: torch.Tensor,
+                             ws: torch.Tensor, perm=None, k: int = 1, stream=None) -> None:
+    """y[r,n] = (wq[e,n] . xq[r]) * xs[r] * wscale[e,n]: xq [R, K] int8 (or the
+    tokens, with perm) with a scale per row, wq [E, N, K] int8 with wscale [E, N],
+    y [R, N] bf16 or fp32."""
+    E, N, K = wq.shape
+    R = y.shape[0]
+    yp, ldy = _rows(y, N, (torch.bfloat16, torch.float32))
+    pp, kk = _gather(xq, R, perm, k)
+    s = _group_shape(R, E, N, K)
+    _check(lib().eaas_grouped_matmul_int8(
+        ctypes.byref(s), _dense(xq, torch.int8, xq.shape[0], K),
+        _dense(xs, torch.float32, xq.shape[0]), pp, kk, _dense(offsets, torch.int32, E + 1),
+        _dense(wq, torch.int8, E, N, K), _dense(wscale, torch.float32, E, N), yp, ldy,
+        _OUT[y.dtype], _p(ws), ws.numel(), _stream(stream)), "eaas_grouped_matmul_int8")
+
+
+def _half(gu: torch.Tensor) -> tuple[int, int]:
+    rows, two = gu.shape
+    if two % 2:
+        raise ValueError("gu holds the gate columns, then as many up columns")
+    return rows, two // 2
+
+
+def _count(n_rows):
+    if n_rows is None:
+        return None
+    return _dense(n_rows.reshape(-1), torch.int32, 1)
+
+
+def eaas_swiglu(gu: torch.Tensor, h: torch.Tensor, n_rows=None, stream=None) -> None:
+    """h = silu(gate) * up: gu [rows, 2I] bf16 (gate, then up), h [rows, I] bf16.
+    n_rows: a device int32 (offsets[E:]) that bounds the rows."""
+    rows, I = _half(gu)
+    _check(lib().eaas_swiglu(_dense(gu, torch.bfloat16, rows, 2 * I), rows, I, _count(n_rows),
+                             _dense(h, torch.bfloat16, rows, I), _stream(stream)), "eaas_swiglu")
+
+
+def eaas_swiglu_int8(gu: torch.Tensor, q: torch.Tensor, s: torch.Tensor, n_rows=None,
+                     stream=None) -> None:
+    """The same as int8 rows q [rows, I] with a scale per row, s [rows] fp32."""
+    rows, I = _half(gu)
+    _check(lib().eaas_swiglu_int8(_dense(gu, torch.bfloat16, rows, 2 * I), rows, I,
+                                  _count(n_rows), _dense(q, torch.int8, rows, I),
+                                  _dense(s, torch.float32, rows), _stream(stream)),
+           "eaas_swiglu_int8")
+
+
+def eaas_swiglu_backward(gu: torch.Tensor, dh: torch.Tensor, dgu: torch.Tensor, n_rows=None,
+                         stream=None) -> None:
+    """dgu [rows, 2I] bf16 (dgate, then dup) from gu and dh [rows, I] bf16; dgu may
+    be gu."""
+    rows, I = _half(gu)
+    _check(lib().eaas_swiglu_backward(_dense(gu, torch.bfloat16, rows, 2 * I),
+                                      _dense(dh, torch.bfloat16, rows, I), rows, I,
+                                      _count(n_rows), _dense(dgu, torch.bfloat16, rows, 2 * I),
+                                      _stream(stream)), "eaas_swiglu_backward")
+
+
+def eaas_unpermute_combine_backward(dout: torch.Tensor, y_perm: torch.Tensor, routing: dict,
+                                    topk_weights: torch.Tensor, dy_perm: torch.Tensor,
+                                    dweights: torch.Tensor, E: int, I: int = 128,
+                                    stream=None) -> None:
+    """Gradients of eaas_unpermute_combine: dout [T, H] bf16 or fp32, y_perm
+    [T*k, H] fp32 -> dy_perm [T*k, H] bf16, dweights [T, k] fp32."""
+    T, k = topk_weights.shape
+    H = dout.shape[1]
+    if dout.dtype not in _OUT or dout.shape[0] != T:
+        raise ValueError(f"dout must be [{T}, H] bf16 or fp32")
+    s = _shape(T, H, I, E, k)
+    r = _routing(routing)
+    _check(lib().eaas_unpermute_combine_backward(
+        ctypes.byref(s), _p(dout), _OUT[dout.dtype], _dense(y_perm, torch.float32, T * k, H),
+        ctypes.byref(r), _dense(topk_weights, torch.float32, T, k),
+        _dense(dy_perm, torch.bfloat16, T * k, H), _dense(dweights, torch.float32, T, k),
+        _stream(stream)), "eaas_unpermute_combine_backward")
