@@ -27,12 +27,15 @@ struct GroupedParams {
   long long ldb;
   const int32_t* perm;    // kForward: rows of a; kGradWeights: rows of b; or nullptr
   int k;                  // slots per token (with perm)
+  uint32_t k_mul;         // slot / k as (slot * k_mul >> 32) >> k_shift, for k > 1
+  int k_shift;
   const int32_t* offsets; // [E+1]
   int R, E, N, K;
   void* out;              // y | dx | dW
   long long ldo;
   bool out_fp32;
   bool vec;               // out may be stored four columns at a time
+  bool vec16;             // and 16 bytes at a time
   bool accumulate;        // kGradWeights: out += (fp32)
   const float* row_scale; // 8-bit integers: of x's rows
   const float* col_scale; // [E,N]
@@ -191,6 +194,10 @@ __device__ __forceinline__ f32x4 scaled(const GroupedParams& p, int e, float rs,
     o[c] = (float)v[c] * rs * (j + c < p.N ? p.col_scale[(size_t)e * p.N + j + c] : 0.0f);
   return o;
 }
+
+// grouped_fast.hip: 256 x 256 tiles, sizes and addresses in multiples of 16 bytes.
+template <int DIR, bool I8>
+hipError_t launch_grouped_pp(const GroupedParams& p, long long tiles, hipStream_t stream);
 
 // Where a partial sum of row i, column j goes (kGradWeights: row n of group e).
 template <int DIR>

@@ -336,12 +336,32 @@ int sum_parts(const GroupedArgs& a) {
   return (int)std::max<long long>(1, std::min<long long>(512 / tiles, steps / 8));
 }
 
+// Whether the loads that go straight to LDS may be used: everything they read in
+// multiples of 16 bytes (rows of W: K elements; the sum of kGradRows: N), and what
+// one descriptor covers below 2 GiB: 256 rows, or with perm all tokens.
+bool in_16_bytes(const GroupedArgs& a) {
+  const int m = a.i8 ? 16 : 8, esz = a.i8 ? 1 : 2;
+  if (a.K % m || a.lda % m || (uintptr_t)a.a % 16 || (uintptr_t)a.b % 16) return false;
+  const long long ldb = a.dir == kGradWeights ? a.ldb : a.K, most = 1LL << 31;
+  if (256 * esz * std::max(a.lda, ldb) >= most) return false;
+  if (a.perm && a.R / a.k * (a.dir == kGradWeights ? ldb : a.lda) * esz >= most) return false;
+  if (a.dir == kForward) return true;
+  return a.N % m == 0 && (a.dir == kGradRows || ldb % m == 0);
+}
+
+// 256 x 256 tiles rather than 128 x 128 through registers.
+bool large_tiles(const GroupedArgs& a) {
+  if (!in_16_bytes(a) || sum_parts(a) > 1) return false;
+  return a.R >= 128LL * a.E && out_tiles(a, 256, 256) >= 192;
+}
+
 template <int DIR, bool I8>
 hipError_t launch_any(GroupedParams p, const GroupedArgs& a, hipStream_t stream) {
   const long long tiles = out_tiles(a, kBI, kBJ);
   if (tiles <= 0) return hipSuccess;
   if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
   p.splits = sum_parts(a);
+  if (large_tiles(a)) return launch_grouped_pp<DIR, I8>(p, out_tiles(a, 256, 256), stream);
   hipLaunchKernelGGL((grouped_any_kernel<DIR, I8>), dim3((unsigned)tiles, (unsigned)p.splits),
                      dim3(kThreads), 0, stream, p);
   hipError_t e = hipGetLastError();
@@ -381,6 +401,11 @@ hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream) {
   p.out_fp32 = a.out_fp32;
   p.accumulate = a.accumulate;
   p.vec = a.ldo % 4 == 0 && (uintptr_t)a.out % (a.out_fp32 ? 16 : 8) == 0;
+  p.vec16 = a.ldo * (a.out_fp32 ? 4 : 2) % 16 == 0 && (uintptr_t)a.out % 16 == 0;
+  int shift = 0;
+  while ((1LL << shift) < a.k) ++shift;
+  p.k_mul = (uint32_t)(((1ULL << (31 + shift)) + a.k - 1) / a.k);
+  p.k_shift = shift - 1;
   p.row_scale = a.row_scale;
   p.col_scale = a.col_scale;
   p.part = a.ws;
