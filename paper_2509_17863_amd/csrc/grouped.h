@@ -53,8 +53,19 @@ __device__ __forceinline__ void group_range(const GroupedParams& p, int e, int& 
   end = min(max(p.offsets[e + 1], beg), p.R);
 }
 
+// The token of a slot.
+__device__ __forceinline__ int token_of(const GroupedParams& p, int slot) {
+  slot = min(max(slot, 0), p.R - 1);
+  return p.k == 1 ? slot : (int)(__umulhi((uint32_t)slot, p.k_mul) >> p.k_shift);
+}
+
 __device__ __forceinline__ int source_row(const GroupedParams& p, int r) {
-  return p.perm ? min(max(p.perm[r], 0), p.R - 1) / p.k : r;
+  return p.perm ? token_of(p, p.perm[r]) : r;
+}
+
+// Two fp32 to bf16, to the nearest, ties to even (one instruction here).
+__device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
 }
 
 // The part of a product that a workgroup computes.
@@ -167,8 +178,8 @@ __device__ __forceinline__ void store4(const GroupedParams& p, int e, int i, int
       *o = DIR == kGradWeights && p.accumulate ? *o + v : v;
     } else {
       u32x2 o;
-      o[0] = pack_bf16x2(v[0], v[1]);
-      o[1] = pack_bf16x2(v[2], v[3]);
+      o[0] = to_bf16x2(v[0], v[1]);
+      o[1] = to_bf16x2(v[2], v[3]);
       *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out) + at) = o;
     }
     return;
@@ -180,7 +191,7 @@ __device__ __forceinline__ void store4(const GroupedParams& p, int e, int i, int
       float* o = static_cast<float*>(p.out) + at + c;
       *o = DIR == kGradWeights && p.accumulate ? *o + v[c] : v[c];
     } else {
-      static_cast<uint16_t*>(p.out)[at + c] = (uint16_t)f32_to_bf16_bits(v[c]);
+      static_cast<uint16_t*>(p.out)[at + c] = (uint16_t)to_bf16x2(v[c], 0.0f);
     }
   }
 }

@@ -23,10 +23,7 @@
 // lies across it as 64 rows of 512 bytes, read with the transposing LDS load.  The
 // loads are bounds-checked buffer loads: whatever lies past the sum's end or past
 // the last row arrives as zeros.
-#include <algorithm>
-#include <type_traits>
-
-#include "grouped.h"
+#include "grouped_fast.h"
 
 namespace eaas {
 namespace {
@@ -37,37 +34,6 @@ constexpr int kStage = 32768;         // bytes of one operand's tile
 constexpr int kSA = 2, kSB = 3;       // stages of A and B
 constexpr int kLds = (kSA + kSB) * kStage;
 constexpr int kInst = 8;              // loads of one wave per tile of its operand
-
-// One wave-wide load of 16 bytes a lane from memory into LDS: lane l reads at
-// rsrc.base + voff(l), or zeros if that is past the descriptor's size, and the
-// bytes land at lds + 16 * l.  Inline assembly, so that the compiler adds no waits
-// of its own; completion is counted with vmcnt.
-__device__ __forceinline__ void load_lds16(const i32x4& rsrc, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
-               :: "v"(voff), "s"(rsrc), "s"(lds) : "memory");
-}
-
-// Raw buffer descriptor of `bytes` bytes from `base` (both wave-uniform).
-__device__ __forceinline__ i32x4 descriptor(const char* base, uint32_t bytes) {
-  const uint64_t v = reinterpret_cast<uint64_t>(base);
-  i32x4 d;
-  d[0] = __builtin_amdgcn_readfirstlane((int)(uint32_t)v);
-  d[1] = __builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32) & 0xffff);
-  d[2] = __builtin_amdgcn_readfirstlane((int)bytes);
-  d[3] = 0x00020000;
-  return d;
-}
-
-// An offset past every descriptor's end: the arrays that a descriptor covers here
-// end below it, so offset and size together never wrap.
-constexpr uint32_t kNowhere = 0x80000000u;
-
-__device__ __forceinline__ int swz_along(int row) { return (row & 7) ^ ((row >> 3) & 1); }
-// The transposing load's 16 lanes take 4 rows x 32 bytes, its 32 lanes 4 rows x 64
-// bytes: the four rows' chunks go to distinct banks in both views (32 banks or 64).
-__device__ __forceinline__ int swz_across(int row) {
-  return ((row & 1) << 2) | (((row >> 1) & 1) * 10);
-}
 
 template <int DIR, bool I8>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -187,8 +153,7 @@ void grouped_pp_kernel(GroupedParams p) {
       uint32_t at[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t slot = (uint32_t)min(max(slots[2 * q + h], 0), p.R - 1);
-        const uint32_t src = p.k == 1 ? slot : __umulhi(slot, p.k_mul) >> p.k_shift;
+        const uint32_t src = token_of(p, slots[2 * q + h]);
         at[h] = 2 * q + h < left ? src * (uint32_t)b_row : kNowhere;
       }
       const uint32_t base = lane < 32 ? at[0] : at[1];
@@ -331,88 +296,9 @@ void grouped_pp_kernel(GroupedParams p) {
     }
   }
 
-  // The results leave through LDS, 32 rows x 64 columns of a wave at a time, so
-  // that whole row segments are stored.  (The last barrier is behind every wave's
-  // fragment reads; a wave's own LDS accesses complete in order.)
-  constexpr int LD = 68;  // a pad of 16 bytes against bank conflicts
-  LDS_AS float* buf = (LDS_AS float*)(smem_raw + wave * (32 * LD * 4));
-  const int col0 = t.j0 + w4 * 64;
-  if (col0 >= cols) return;
-  if (DIR == kGradWeights && p.accumulate && p.splits == 1 && t.end == t.beg) return;  // + 0
-  // one block row's accumulators to LDS
-  auto stage = [&](const Acc (&a)[NBW]) {
-#pragma unroll
-    for (int j = 0; j < NBW; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        typename std::conditional<I8, i32x4, f32x4>::type o = {a[j][4 * q], a[j][4 * q + 1],
-                                                               a[j][4 * q + 2], a[j][4 * q + 3]};
-        *reinterpret_cast<LDS_AS f32x4*>(buf + lrow * LD + j * 32 + 8 * q + 4 * khalf) =
-            __builtin_bit_cast(f32x4, o);
-      }
-  };
-  auto finished = [&](int row, int col, f32x4 v) {
-    if constexpr (I8)
-      return scaled(p, t.e, p.row_scale[source_row(p, row)], col, __builtin_bit_cast(i32x4, v));
-    else
-      return v;
-  };
-  if (p.splits == 1 && p.vec16 && !p.out_fp32) {
-    // bf16: 8 lanes to a row of 64 results
-    const int cl = (lane & 7) * 8, col = col0 + cl;
-#pragma unroll
-    for (int i = 0; i < MBW; ++i) {
-      stage(acc[i]);
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int m = s * 8 + (lane >> 3);
-        const int ri = grp * 128 + i * 32 + m, row = t.i0 + ri;
-        f32x4 lo = *reinterpret_cast<const LDS_AS f32x4*>(buf + m * LD + cl);
-        f32x4 hi = *reinterpret_cast<const LDS_AS f32x4*>(buf + m * LD + cl + 4);
-        if (ri >= t.i_valid || col >= cols) continue;
-        lo = finished(row, col, lo);
-        hi = finished(row, col + 4, hi);
-        if (col + 8 <= cols) {
-          u32x4 o;
-          o[0] = pack_bf16x2(lo[0], lo[1]);
-          o[1] = pack_bf16x2(lo[2], lo[3]);
-          o[2] = pack_bf16x2(hi[0], hi[1]);
-          o[3] = pack_bf16x2(hi[2], hi[3]);
-          const size_t at = (DIR == kGradWeights ? (size_t)t.e * p.N + row : (size_t)row) * p.ldo;
-          *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.out) + at + col) = o;
-        } else {
-          store4<DIR>(p, t.e, row, col, lo);
-          if (col + 4 < cols) store4<DIR>(p, t.e, row, col + 4, hi);
-        }
-      }
-    }
-  } else {
-    // 16 lanes to a row
-    const int cl = (lane & 15) * 4, col = col0 + cl;
-#pragma unroll
-    for (int i = 0; i < MBW; ++i) {
-      stage(acc[i]);
-#pragma unroll
-      for (int s = 0; s < 8; ++s) {
-        const int m = s * 4 + (lane >> 4);
-        const int ri = grp * 128 + i * 32 + m, row = t.i0 + ri;
-        const f32x4 v = *reinterpret_cast<const LDS_AS f32x4*>(buf + m * LD + cl);
-        if (ri >= t.i_valid || col >= cols) continue;
-        if (p.splits > 1) {
-          float* o = static_cast<float*>(p.part) + part_at<DIR>(p, split, t.e, row, col);
-          if (cols % 4 == 0) {
-            *reinterpret_cast<f32x4*>(o) = v;
-          } else {
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-              if (col + c < cols) o[c] = v[c];
-          }
-        } else {
-          store4<DIR>(p, t.e, row, col, finished(row, col, v));
-        }
-      }
-    }
-  }
+  // (the last barrier is behind every wave's fragment reads)
+  way_out<DIR, I8>(p, t, split, grp * 128, t.j0 + w4 * 64, acc,
+                   (LDS_AS float*)(smem_raw + wave * kWayOutBytes));
 }
 
 }  // namespace
