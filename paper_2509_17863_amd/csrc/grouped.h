@@ -166,6 +166,18 @@ __device__ __forceinline__ bool find_tile(const GroupedParams& p, int* lds, Grou
   }
 }
 
+// Column j of row i of the result.
+template <int DIR>
+__device__ __forceinline__ void store1(const GroupedParams& p, int e, int i, int j, float v) {
+  const size_t at = (DIR == kGradWeights ? ((size_t)e * p.N + i) : (size_t)i) * p.ldo + j;
+  if (p.out_fp32) {
+    float* o = static_cast<float*>(p.out) + at;
+    *o = DIR == kGradWeights && p.accumulate ? *o + v : v;
+  } else {
+    static_cast<uint16_t*>(p.out)[at] = (uint16_t)to_bf16x2(v, 0.0f);
+  }
+}
+
 // Four consecutive columns j.. of row i of the result (row of y or dx, or row n
 // of dW[e]); cols: columns that exist.
 template <int DIR>
@@ -185,15 +197,8 @@ __device__ __forceinline__ void store4(const GroupedParams& p, int e, int i, int
     return;
   }
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    if (j + c >= cols) break;
-    if (p.out_fp32) {
-      float* o = static_cast<float*>(p.out) + at + c;
-      *o = DIR == kGradWeights && p.accumulate ? *o + v[c] : v[c];
-    } else {
-      static_cast<uint16_t*>(p.out)[at + c] = (uint16_t)to_bf16x2(v[c], 0.0f);
-    }
-  }
+  for (int c = 0; c < 4; ++c)
+    if (j + c < cols) store1<DIR>(p, e, i, j + c, v[c]);
 }
 
 // Scales of the 8-bit product at row i and columns j..: the sum rounded to fp32,
@@ -209,6 +214,11 @@ __device__ __forceinline__ f32x4 scaled(const GroupedParams& p, int e, float rs,
 // grouped_fast.hip: 256 x 256 tiles, sizes and addresses in multiples of 16 bytes.
 template <int DIR, bool I8>
 hipError_t launch_grouped_pp(const GroupedParams& p, long long tiles, hipStream_t stream);
+
+// grouped_few.hip: tiles of `rows` (16, 32 or 64) x 64 under the same condition.
+template <int DIR, bool I8>
+hipError_t launch_grouped_few(const GroupedParams& p, int rows, long long tiles,
+                              hipStream_t stream);
 
 // Where a partial sum of row i, column j goes (kGradWeights: row n of group e).
 template <int DIR>

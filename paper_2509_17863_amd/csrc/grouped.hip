@@ -13,18 +13,13 @@
 // lane four elements of its column.
 #include <algorithm>
 
-#include "grouped.h"
+#include "grouped_fast.h"
 
 namespace eaas {
 namespace {
 
 constexpr int kBI = 128, kBJ = 128, kThreads = 256;
 constexpr int kStage = 16384;  // bytes of one operand's tile
-
-__device__ __forceinline__ int swz_along(int row) { return (row & 7) ^ ((row >> 3) & 1); }
-// the transposing load's 16 lanes take 4 rows x 32 bytes: neighbouring rows go
-// to different quarters of the 256 bytes that all banks span
-__device__ __forceinline__ int swz_across(int row) { return (row & 3) << 2; }
 
 // 16 bytes at an address of element alignment.
 __device__ __forceinline__ u32x4 load16(const char* p) {
@@ -153,7 +148,9 @@ __global__ __launch_bounds__(kThreads) void grouped_any_kernel(GroupedParams p) 
   constexpr int ESZ = I8 ? 1 : 2;
   constexpr int SUM = 128 / ESZ;  // the sum's elements in a tile
   static_assert(!I8 || DIR == kForward, "8-bit integers: forward only");
-  __shared__ __attribute__((aligned(16))) char smem[4 * kStage];
+  constexpr int kWaves = kThreads / kWave;
+  constexpr int kLds = std::max(4 * kStage, kWaves * kWayOutBytes);
+  __shared__ __attribute__((aligned(16))) char smem[kLds];
   __shared__ int s_find[kThreads / kWave + 4];
   GroupedTile t;
   if (!find_tile<DIR, kBI, kBJ, kThreads>(p, s_find, t)) return;
@@ -235,44 +232,9 @@ __global__ __launch_bounds__(kThreads) void grouped_any_kernel(GroupedParams p) 
     }
   }
 
-  // acc[i][j][v]: row i*32 + lane % 32, column j*32 + 8*(v/4) + 4*(lane/32) + v % 4
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int ri = wi + 32 * i + (lane & 31);
-    if (ri >= t.i_valid) continue;
-    const int row = t.i0 + ri;
-    float rs = 0.0f;
-    if constexpr (I8) rs = p.row_scale[source_row(p, row)];
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int col = t.j0 + wj + 32 * j + 8 * q + 4 * (lane >> 5);
-        if (col >= cols) continue;
-        if (p.splits > 1) {
-          const size_t at = part_at<DIR>(p, split, t.e, row, col);
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (col + c < cols) {
-              if constexpr (I8) static_cast<int*>(p.part)[at + c] = acc[i][j][4 * q + c];
-              else static_cast<float*>(p.part)[at + c] = acc[i][j][4 * q + c];
-            }
-          continue;
-        }
-        if constexpr (I8) {
-          i32x4 v;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) v[c] = acc[i][j][4 * q + c];
-          store4<DIR>(p, t.e, row, col, scaled(p, t.e, rs, col, v));
-        } else {
-          f32x4 v;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) v[c] = acc[i][j][4 * q + c];
-          store4<DIR>(p, t.e, row, col, v);
-        }
-      }
-  }
+  // (the last barrier is behind every wave's fragment reads)
+  way_out<DIR, I8>(p, t, split, wi, t.j0 + wj, acc,
+                   (LDS_AS float*)(smem + wave * kWayOutBytes));
 }
 
 // The parts of a split sum joined, in ascending order: one thread for four
@@ -326,16 +288,6 @@ long long out_tiles(const GroupedArgs& a, int bi, int bj) {
   return (long long)a.E * ceil_div(a.N, bi) * ceil_div(a.K, bj);
 }
 
-// Parts of the sum: where the tiles alone leave most of the 256 CUs idle, as
-// many as give two workgroups to a CU, of at least 8 tiles of the sum each.
-int sum_parts(const GroupedArgs& a) {
-  const long long tiles = out_tiles(a, kBI, kBJ);
-  const int sum = a.dir == kForward ? a.K : a.dir == kGradRows ? a.N : a.R;
-  const int steps = ceil_div(sum, a.i8 ? 128 : 64);
-  if (tiles >= 192 || steps < 16) return 1;
-  return (int)std::max<long long>(1, std::min<long long>(512 / tiles, steps / 8));
-}
-
 // Whether the loads that go straight to LDS may be used: everything they read in
 // multiples of 16 bytes (rows of W: K elements; the sum of kGradRows: N), and what
 // one descriptor covers below 2 GiB: 256 rows, or with perm all tokens.
@@ -349,22 +301,60 @@ bool in_16_bytes(const GroupedArgs& a) {
   return a.N % m == 0 && (a.dir == kGradRows || ldb % m == 0);
 }
 
-// 256 x 256 tiles rather than 128 x 128 through registers.
-bool large_tiles(const GroupedArgs& a) {
-  if (!in_16_bytes(a) || sum_parts(a) > 1) return false;
-  return a.R >= 128LL * a.E && out_tiles(a, 256, 256) >= 192;
+// Which kernel computes a product, on which tiles, and in how many parts.
+enum GroupedKernel { kAny, kFew, kLarge };
+struct GroupedPlan {
+  GroupedKernel kernel;
+  int bi, bj;
+  int splits;
+};
+
+// Parts of the sum: where the tiles leave most of the chip idle, as many as make
+// `enough` workgroups, of at least `least` tiles of the sum each.
+int sum_parts(const GroupedArgs& a, long long tiles, int enough, int least) {
+  const int sum = a.dir == kForward ? a.K : a.dir == kGradRows ? a.N : a.R;
+  const int steps = ceil_div(sum, a.i8 ? 128 : 64);
+  if (tiles <= 0 || tiles * 8 >= 3 * enough) return 1;
+  return (int)std::max<long long>(1, std::min<long long>(enough / tiles, steps / least));
+}
+
+GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
+  const long long rows = a.R / std::max(1, std::min(a.R, a.E));  // of a group that has any
+  if (in16 && a.dir != kGradWeights && rows <= 64) {
+    GroupedPlan g{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};
+    g.splits = sum_parts(a, out_tiles(a, g.bi, g.bj), 512, 8);
+    return g;
+  }
+  const long long tiles = out_tiles(a, kBI, kBJ);
+  GroupedPlan g{kAny, kBI, kBJ, sum_parts(a, tiles, 512, 8)};
+  if (in16 && g.splits == 1 && rows >= 128 && out_tiles(a, 256, 256) >= 192)
+    g = GroupedPlan{kLarge, 256, 256, 1};
+  return g;
+}
+
+size_t part_bytes(const GroupedArgs& a, const GroupedPlan& g) {
+  if (g.splits == 1) return 0;
+  const size_t rows = a.dir == kGradWeights ? (size_t)a.E * a.N : (size_t)a.R;
+  return (size_t)g.splits * rows * (a.dir == kForward ? a.N : a.K) * 4;
 }
 
 template <int DIR, bool I8>
-hipError_t launch_any(GroupedParams p, const GroupedArgs& a, hipStream_t stream) {
-  const long long tiles = out_tiles(a, kBI, kBJ);
+hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t stream) {
+  const GroupedPlan g = grouped_plan(a, in_16_bytes(a));
+  const long long tiles = out_tiles(a, g.bi, g.bj);
   if (tiles <= 0) return hipSuccess;
   if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
-  p.splits = sum_parts(a);
-  if (large_tiles(a)) return launch_grouped_pp<DIR, I8>(p, out_tiles(a, 256, 256), stream);
-  hipLaunchKernelGGL((grouped_any_kernel<DIR, I8>), dim3((unsigned)tiles, (unsigned)p.splits),
-                     dim3(kThreads), 0, stream, p);
-  hipError_t e = hipGetLastError();
+  p.splits = g.splits;
+  hipError_t e = hipSuccess;
+  if (g.kernel == kLarge) {
+    e = launch_grouped_pp<DIR, I8>(p, tiles, stream);
+  } else if (g.kernel == kFew) {
+    if constexpr (DIR != kGradWeights) e = launch_grouped_few<DIR, I8>(p, g.bi, tiles, stream);
+  } else {
+    hipLaunchKernelGGL((grouped_any_kernel<DIR, I8>), dim3((unsigned)tiles, (unsigned)p.splits),
+                       dim3(kThreads), 0, stream, p);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || p.splits == 1) return e;
   const long long rows = DIR == kGradWeights ? (long long)a.E * a.N : a.R;
   const long long quads = rows * ceil_div(DIR == kForward ? a.N : a.K, 4);
@@ -377,10 +367,11 @@ hipError_t launch_any(GroupedParams p, const GroupedArgs& a, hipStream_t stream)
 }  // namespace
 
 size_t grouped_workspace(const GroupedArgs& a) {
-  const int parts = sum_parts(a);
-  if (parts == 1) return 0;
-  const size_t rows = a.dir == kGradWeights ? (size_t)a.E * a.N : (size_t)a.R;
-  return (size_t)parts * rows * (a.dir == kForward ? a.N : a.K) * 4;
+  return part_bytes(a, grouped_plan(a, in_16_bytes(a)));
+}
+
+size_t grouped_workspace_most(const GroupedArgs& a) {
+  return std::max(part_bytes(a, grouped_plan(a, true)), part_bytes(a, grouped_plan(a, false)));
 }
 
 hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream) {
@@ -409,10 +400,10 @@ hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream) {
   p.row_scale = a.row_scale;
   p.col_scale = a.col_scale;
   p.part = a.ws;
-  if (a.i8) return launch_any<kForward, true>(p, a, stream);
-  if (a.dir == kForward) return launch_any<kForward, false>(p, a, stream);
-  if (a.dir == kGradRows) return launch_any<kGradRows, false>(p, a, stream);
-  return launch_any<kGradWeights, false>(p, a, stream);
+  if (a.i8) return launch_product<kForward, true>(p, a, stream);
+  if (a.dir == kForward) return launch_product<kForward, false>(p, a, stream);
+  if (a.dir == kGradRows) return launch_product<kGradRows, false>(p, a, stream);
+  return launch_product<kGradWeights, false>(p, a, stream);
 }
 
 }  // namespace eaas

@@ -121,8 +121,8 @@ size_t eaas_grouped_workspace_bytes(const eaas_group_shape* s) {
   if (check_group(s) != EAAS_OK) return 0;
   size_t n = 256;
   for (int dir = kForward; dir <= kGradWeights; ++dir)
-    n = std::max(n, grouped_workspace(args_of(s, dir, false)));
-  n = std::max(n, grouped_workspace(args_of(s, kForward, true)));
+    n = std::max(n, grouped_workspace_most(args_of(s, dir, false)));
+  n = std::max(n, grouped_workspace_most(args_of(s, kForward, true)));
   return (n + 255) / 256 * 256;
 }
 

@@ -1,6 +1,5 @@
-// Parts of the grouped product kernels that load straight into LDS
-// (grouped_fast.hip): the loads, the order of chunks in LDS, and
-// the way out of the results.
+// Parts shared by the grouped product kernels: loads straight into LDS, the order
+// of chunks there, and the way out of the results.
 #pragma once
 
 #include <type_traits>
@@ -60,8 +59,11 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
   const int cols = columns<DIR>(p);
   if (col0 >= cols) return;
   if (DIR == kGradWeights && p.accumulate && p.splits == 1 && t.end == t.beg) return;  // + 0
-  const bool narrow = p.splits == 1 && p.vec16 && !p.out_fp32;  // bf16, 16 bytes at a time
-  const int cl = narrow ? (lane & 7) * 8 : (lane & 15) * 4, col = col0 + cl;
+  // how rows are stored: as bf16 or fp32, 16 bytes a lane, or an element a lane
+  // where the result's rows are not in multiples of 16 bytes
+  const bool loose = p.splits == 1 ? !p.vec16 : cols % 4 != 0;
+  const bool narrow = !loose && p.splits == 1 && !p.out_fp32;
+  const int cl = loose ? lane : narrow ? (lane & 7) * 8 : (lane & 15) * 4, col = col0 + cl;
   // 8-bit integers: rows are scaled on the way into LDS, columns on the way out
   const bool scale = I8 && p.splits == 1;
   float rs[MBW], cs[8];
@@ -125,6 +127,21 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
           if (col + 4 < cols) store4<DIR>(p, t.e, row, col + 4, hi);
         }
       }
+    } else if (loose) {
+      if (col < cols) {
+#pragma unroll
+        for (int m = 0; m < 32; ++m) {
+          const int ri = row0 + i * 32 + m, row = t.i0 + ri;
+          float v = from[m * LD];
+          if (ri >= t.i_valid) continue;
+          if (p.splits > 1) {
+            static_cast<float*>(p.part)[part_at<DIR>(p, split, t.e, row, col)] = v;
+          } else {
+            if constexpr (I8) v *= cs[0];
+            store1<DIR>(p, t.e, row, col, v);
+          }
+        }
+      }
     } else {
       // 16 lanes to a row
 #pragma unroll
@@ -134,26 +151,20 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
         f32x4 v = *reinterpret_cast<const LDS_AS f32x4*>(from + m * LD);
         if (ri >= t.i_valid || col >= cols) continue;
         if (p.splits > 1) {
-          float* o = static_cast<float*>(p.part) + part_at<DIR>(p, split, t.e, row, col);
-          if (cols % 4 == 0) {
-            *reinterpret_cast<f32x4*>(o) = v;
-          } else {
+          *reinterpret_cast<f32x4*>(static_cast<float*>(p.part) +
+                                    part_at<DIR>(p, split, t.e, row, col)) = v;
+          continue;
+        }
+        if constexpr (I8) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-              if (col + c < cols) o[c] = v[c];
-          }
+          for (int c = 0; c < 4; ++c) v[c] *= cs[c];
+        }
+        if (col + 4 <= cols && !p.accumulate) {
+          const size_t at = (DIR == kGradWeights ? (size_t)t.e * p.N + row : (size_t)row) * p.ldo;
+          __builtin_nontemporal_store(
+              v, reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at + col));
         } else {
-          if constexpr (I8) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] *= cs[c];
-          }
-          if (p.vec16 && p.out_fp32 && col + 4 <= cols && !p.accumulate) {
-            const size_t at = (DIR == kGradWeights ? (size_t)t.e * p.N + row : (size_t)row) * p.ldo;
-            __builtin_nontemporal_store(
-                v, reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + at + col));
-          } else {
-            store4<DIR>(p, t.e, row, col, v);
-          }
+          store4<DIR>(p, t.e, row, col, v);
         }
       }
     }

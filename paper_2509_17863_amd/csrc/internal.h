@@ -165,7 +165,9 @@ struct GroupedArgs {
   const float* col_scale;
   void* ws;                 // grouped_workspace bytes
 };
-size_t grouped_workspace(const GroupedArgs& a);  // (a's sizes only)
+size_t grouped_workspace(const GroupedArgs& a);
+// At most, for any strides and alignment (a's sizes only).
+size_t grouped_workspace_most(const GroupedArgs& a);
 hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream);
 
 // Activation, 8-bit rows and the combine's gradient (activation.hip).
