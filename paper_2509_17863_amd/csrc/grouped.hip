@@ -5,9 +5,11 @@
 // A workgroup of four waves computes a tile of 128 x 128 results; a wave holds
 // 64 x 64 of them as 2 x 2 blocks of v_mfma_f32_32x32x16_bf16 (8-bit integers:
 // v_mfma_i32_32x32x32_i8).  Tiles of both operands, 16 KiB each, pass through
-// registers into one of two LDS stages while the other is multiplied: loads into
-// registers take any byte alignment, and what lies past an edge is replaced by
-// zeros there.  An operand that lies along the sum is kept as rows of 128 bytes
+// registers into LDS: loads into registers take any byte alignment, and what lies
+// past an edge is replaced by zeros there.  The next tile's loads are in flight
+// while a tile is multiplied; three workgroups to a CU cover the rest of their time
+// (one LDS stage each: with two stages and two workgroups the products of odd sizes
+// ran a third slower).  An operand that lies along the sum is kept as rows of 128 bytes
 // and read back 16 bytes a lane; one that lies across it is kept as it comes, 64
 // rows of 128 columns, and read with the transposing LDS load, which hands each
 // lane four elements of its column.
@@ -28,18 +30,21 @@ __device__ __forceinline__ u32x4 load16(const char* p) {
   return v;
 }
 
-// The first n elements of 16 bytes, zeros after them.
+// The first n >= 1 elements of 16 bytes, zeros after them.  (Every lane loads as
+// many elements as fit, the last one repeatedly: loads under a condition each would
+// be waited for one by one.)
 template <int ESZ>
 __device__ __forceinline__ u32x4 load_some(const char* p, int n) {
+  constexpr int EPC = 16 / ESZ;
+  uint32_t e[EPC];
+#pragma unroll
+  for (int c = 0; c < EPC; ++c) {
+    const char* at = p + min(c, n - 1) * ESZ;
+    e[c] = ESZ == 2 ? *reinterpret_cast<const uint16_t*>(at) : *reinterpret_cast<const uint8_t*>(at);
+  }
   u32x4 v = {0, 0, 0, 0};
 #pragma unroll
-  for (int c = 0; c < 16 / ESZ; ++c) {
-    if (c >= n) break;
-    const uint32_t b = ESZ == 2 ? *reinterpret_cast<const uint16_t*>(p + 2 * c)
-                                : *reinterpret_cast<const uint8_t*>(p + c);
-    const int at = c * ESZ;
-    v[at / 4] |= b << (8 * (at % 4));
-  }
+  for (int c = 0; c < EPC; ++c) v[c * ESZ / 4] |= (c < n ? e[c] : 0u) << (8 * (c * ESZ % 4));
   return v;
 }
 
@@ -143,13 +148,14 @@ __device__ __forceinline__ u32x4 fragment(const LDS_AS char* stage, int c0, int 
 }
 
 template <int DIR, bool I8>
-__global__ __launch_bounds__(kThreads) void grouped_any_kernel(GroupedParams p) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3)))
+void grouped_any_kernel(GroupedParams p) {
   constexpr bool A_ACROSS = DIR == kGradWeights, B_ACROSS = DIR != kForward;
   constexpr int ESZ = I8 ? 1 : 2;
   constexpr int SUM = 128 / ESZ;  // the sum's elements in a tile
   static_assert(!I8 || DIR == kForward, "8-bit integers: forward only");
   constexpr int kWaves = kThreads / kWave;
-  constexpr int kLds = std::max(4 * kStage, kWaves * kWayOutBytes);
+  constexpr int kLds = std::max(2 * kStage, kWaves * kWayOutHalf * 4);
   __shared__ __attribute__((aligned(16))) char smem[kLds];
   __shared__ int s_find[kThreads / kWave + 4];
   GroupedTile t;
@@ -195,14 +201,12 @@ __global__ __launch_bounds__(kThreads) void grouped_any_kernel(GroupedParams p) 
 
   if (first < last) {
     load(first);
-    la.store(lds);
-    lb.store(lds + kStage);
-    __syncthreads();
     for (int kt = first; kt < last; ++kt) {
-      const int cur = (kt - first) & 1;
+      la.store(lds);
+      lb.store(lds + kStage);
+      __syncthreads();
       if (kt + 1 < last) load(kt + 1);
-      const LDS_AS char* sa = lds + cur * 2 * kStage;
-      const LDS_AS char* sb = sa + kStage;
+      const LDS_AS char *sa = lds, *sb = lds + kStage;
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         u32x4 fa[2], fb[2];
@@ -224,17 +228,13 @@ __global__ __launch_bounds__(kThreads) void grouped_any_kernel(GroupedParams p) 
                   0, 0, 0);
           }
       }
-      if (kt + 1 < last) {
-        la.store(lds + (cur ^ 1) * 2 * kStage);
-        lb.store(lds + (cur ^ 1) * 2 * kStage + kStage);
-      }
       __syncthreads();
     }
   }
 
   // (the last barrier is behind every wave's fragment reads)
-  way_out<DIR, I8>(p, t, split, wi, t.j0 + wj, acc,
-                   (LDS_AS float*)(smem + wave * kWayOutBytes));
+  way_out<DIR, I8, 1>(p, t, split, wi, t.j0 + wj, acc,
+                      (LDS_AS float*)smem + wave * kWayOutHalf);
 }
 
 // The parts of a split sum joined, in ascending order: one thread for four

@@ -41,15 +41,15 @@ __device__ __forceinline__ int swz_across(int row) {
 
 // A wave's results, MBW x 2 blocks of 32 x 32, to memory: rows row0.. of the tile,
 // columns col0.. of the result.  They pass through `buf`, kWayOutBytes of LDS that
-// this wave alone uses, 32 rows x 64 columns at a time in two halves in turn, so
-// that whole row segments are stored.  acc[i][j][v]: row i*32 + lane % 32, column
+// this wave alone uses, 32 rows x 64 columns at a time (in two halves in turn, if
+// there is LDS for both), so that whole row segments are stored.  acc[i][j][v]: row i*32 + lane % 32, column
 // j*32 + 8*(v/4) + 4*(lane/32) + v % 4.  (A wave's own LDS accesses complete in
 // order.)
 constexpr int kWayOutLd = 68;  // floats: a pad of 16 bytes against bank conflicts
 constexpr int kWayOutHalf = 32 * kWayOutLd;
 constexpr int kWayOutBytes = 2 * kWayOutHalf * 4;
 
-template <int DIR, bool I8, int MBW, class Acc>
+template <int DIR, bool I8, int HALVES, int MBW, class Acc>
 __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTile& t, int split,
                                         int row0, int col0, const Acc (&acc)[MBW][2],
                                         LDS_AS float* buf) {
@@ -76,7 +76,7 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
       cs[c] = p.col_scale[(size_t)t.e * p.N + min(col + c, p.N - 1)];
   }
   auto stage = [&](int i) {
-    LDS_AS float* at = buf + (i & 1) * kWayOutHalf + lrow * LD + 4 * khalf;
+    LDS_AS float* at = buf + (i % HALVES) * kWayOutHalf + lrow * LD + 4 * khalf;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -91,11 +91,12 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
         *reinterpret_cast<LDS_AS f32x4*>(at + j * 32 + 8 * q) = o;
       }
   };
-  stage(0);
+  if (HALVES == 2) stage(0);
 #pragma unroll
   for (int i = 0; i < MBW; ++i) {
-    if (i + 1 < MBW) stage(i + 1);
-    const LDS_AS float* from = buf + (i & 1) * kWayOutHalf + cl;
+    if (HALVES == 1) stage(i);
+    else if (i + 1 < MBW) stage(i + 1);
+    const LDS_AS float* from = buf + (i % HALVES) * kWayOutHalf + cl;
     if (narrow) {
       // 8 lanes to a row of 64 results
 #pragma unroll
@@ -128,18 +129,36 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
         }
       }
     } else if (loose) {
-      if (col < cols) {
+      // 64 lanes to a row; rows that exist are a prefix
+      const int live = min(32, t.i_valid - (row0 + i * 32));
+      const int row = t.i0 + row0 + i * 32;
+      if (col < cols && live > 0) {
+        auto rows = [&](auto* out, size_t ld, auto convert) {
+#pragma unroll 1
+          for (int m0 = 0; m0 < live; m0 += 8) {
+            float v[8];
 #pragma unroll
-        for (int m = 0; m < 32; ++m) {
-          const int ri = row0 + i * 32 + m, row = t.i0 + ri;
-          float v = from[m * LD];
-          if (ri >= t.i_valid) continue;
-          if (p.splits > 1) {
-            static_cast<float*>(p.part)[part_at<DIR>(p, split, t.e, row, col)] = v;
-          } else {
-            if constexpr (I8) v *= cs[0];
-            store1<DIR>(p, t.e, row, col, v);
+            for (int m = 0; m < 8; ++m) v[m] = from[(m0 + m) * LD];
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+              if (m0 + m < live) convert(out + (m0 + m) * ld, v[m]);
           }
+        };
+        if (p.splits > 1) {
+          rows(static_cast<float*>(p.part) + part_at<DIR>(p, split, t.e, row, col), cols,
+               [](float* o, float v) { *o = v; });
+        } else {
+          const size_t at =
+              (DIR == kGradWeights ? (size_t)t.e * p.N + row : (size_t)row) * p.ldo + col;
+          const float c = I8 ? cs[0] : 1.0f;
+          if (!p.out_fp32)
+            rows(static_cast<uint16_t*>(p.out) + at, p.ldo,
+                 [c](uint16_t* o, float v) { *o = (uint16_t)to_bf16x2(I8 ? v * c : v, 0.0f); });
+          else if (p.accumulate)
+            rows(static_cast<float*>(p.out) + at, p.ldo, [](float* o, float v) { *o += v; });
+          else
+            rows(static_cast<float*>(p.out) + at, p.ldo,
+                 [c](float* o, float v) { *o = I8 ? v * c : v; });
         }
       }
     } else {

@@ -297,7 +297,7 @@ void grouped_pp_kernel(GroupedParams p) {
   }
 
   // (the last barrier is behind every wave's fragment reads)
-  way_out<DIR, I8>(p, t, split, grp * 128, t.j0 + w4 * 64, acc,
+  way_out<DIR, I8, 2>(p, t, split, grp * 128, t.j0 + w4 * 64, acc,
                    (LDS_AS float*)(smem_raw + wave * kWayOutBytes));
 }
 
