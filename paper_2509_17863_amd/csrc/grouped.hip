@@ -69,7 +69,7 @@ struct Loader {
       chunk = tid & 7;
       r0 = tid >> 3;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) row[q] = rp(r0 + 32 * q);
+      for (int q = 0; q < 4; ++q) row[q] = rp(q, r0 + 32 * q);
     }
   }
   // s0: the sum's index where the tile starts; s_end: where the sum ends
@@ -82,11 +82,11 @@ struct Loader {
       for (int q = 0; q < 4; ++q) {
         const int s = s0 + r0 + 16 * q;
         if (inside) {
-          v[q] = load16(rp(s) + (size_t)c * ESZ);
+          v[q] = load16(rp(q, s) + (size_t)c * ESZ);
         } else {
           v[q] = u32x4{0, 0, 0, 0};
           if (s < s_end && c < width) {
-            const char* p = rp(s) + (size_t)c * ESZ;
+            const char* p = rp(q, s) + (size_t)c * ESZ;
             v[q] = c + EPC <= width ? load16(p) : load_some<ESZ>(p, width - c);
           }
         }
@@ -170,15 +170,23 @@ void grouped_any_kernel(GroupedParams p) {
 
   const char* w = p.b + (DIR == kGradWeights ? 0 : (size_t)t.e * p.N * p.K * ESZ);
   // rows past the tile's repeat one that exists; their results are not stored
-  auto a_row = [&](int i) {
+  auto a_row = [&](int, int i) {
     if (DIR == kGradWeights) return p.a + (size_t)(t.beg + i) * p.lda * ESZ;
     const int r = t.i0 + min(i, t.i_valid - 1);
     return p.a + (size_t)(DIR == kForward ? source_row(p, r) : r) * p.lda * ESZ;
   };
-  auto b_row = [&](int j) {
+  int src[4];  // kGradWeights: this thread's rows of x in the next tile to load
+  auto b_row = [&](int q, int j) {
     if (DIR == kForward) return w + (size_t)min(t.j0 + j, cols - 1) * p.ldb * ESZ;
     if (DIR == kGradRows) return w + (size_t)j * p.ldb * ESZ;
-    return w + (size_t)source_row(p, t.beg + j) * p.ldb * ESZ;
+    return w + (size_t)src[q] * p.ldb * ESZ;
+  };
+  auto find_rows = [&](int kt) {
+    if constexpr (DIR == kGradWeights) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        src[q] = source_row(p, min(t.beg + kt * SUM + (int)threadIdx.x / 16 + 16 * q, t.end - 1));
+    }
   };
   Loader<A_ACROSS, ESZ> la;
   Loader<B_ACROSS, ESZ> lb;
@@ -187,6 +195,7 @@ void grouped_any_kernel(GroupedParams p) {
   auto load = [&](int kt) {
     la.load(a_row, kt * SUM, sum_end, t.i0, p.N);
     lb.load(b_row, kt * SUM, sum_end, t.j0, cols);
+    if (kt + 1 < last) find_rows(kt + 1);
   };
 
   typedef typename std::conditional<I8, i32x16, f32x16>::type Acc;
@@ -200,6 +209,7 @@ void grouped_any_kernel(GroupedParams p) {
   LDS_AS char* lds = (LDS_AS char*)smem;
 
   if (first < last) {
+    find_rows(first);
     load(first);
     for (int kt = first; kt < last; ++kt) {
       la.store(lds);
@@ -238,27 +248,44 @@ void grouped_any_kernel(GroupedParams p) {
 }
 
 // The parts of a split sum joined, in ascending order: one thread for four
-// columns of one row.
-template <int DIR, bool I8>
+// columns of one row (VEC: rows of whole quads, 16 bytes a part).  Parts are loaded
+// eight at a time.
+template <int DIR, bool I8, bool VEC>
 __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p) {
+  typedef typename std::conditional<I8, i32x4, f32x4>::type Quad;
+  typedef typename std::conditional<I8, int, float>::type One;
   const int cols = columns<DIR>(p);
   const int quads = ceil_div(cols, 4);
   const long long rows = DIR == kGradWeights ? (long long)p.E * p.N
                                              : min(max(p.offsets[p.E], 0), p.R);
   const long long first = DIR == kGradWeights ? 0 : min(max(p.offsets[0], 0), p.R);
+  const size_t stride = (DIR == kGradWeights ? (size_t)p.E * p.N : (size_t)p.R) * cols;
   for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (rows - first) * quads;
        u += (long long)gridDim.x * 256) {
     const long long row = first + u / quads;
     const int j = (int)(u % quads) * 4;
+    const One* part = static_cast<const One*>(p.part) + (size_t)row * cols + j;
+    Quad v = {0, 0, 0, 0};
+    for (int s0 = 0; s0 < p.splits; s0 += 8) {
+      Quad t[8];
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        const One* at = part + (size_t)min(s0 + s, p.splits - 1) * stride;
+        if constexpr (VEC) {
+          t[s] = *reinterpret_cast<const Quad*>(at);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) t[s][c] = at[min(c, cols - 1 - j)];
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        if (s0 + s < p.splits) v += t[s];
+    }
     const int e = DIR == kGradWeights ? (int)(row / p.N) : 0;
     const int i = DIR == kGradWeights ? (int)(row % p.N) : (int)row;
     if constexpr (I8) {
-      i32x4 v = {0, 0, 0, 0};
-      for (int s = 0; s < p.splits; ++s)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (j + c < cols) v[c] += static_cast<const int*>(p.part)[part_at<DIR>(p, s, e, i, j + c)];
-      // the group whose rows hold i: the last that starts at or before it and is not empty
+      // the group whose rows hold i: the last that starts at or before it
       int lo = 0, hi = p.E - 1;
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
@@ -266,12 +293,6 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p) {
       }
       store4<DIR>(p, lo, i, j, scaled(p, lo, p.row_scale[source_row(p, i)], j, v));
     } else {
-      f32x4 v = {0, 0, 0, 0};
-      for (int s = 0; s < p.splits; ++s)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (j + c < cols)
-            v[c] += static_cast<const float*>(p.part)[part_at<DIR>(p, s, e, i, j + c)];
       store4<DIR>(p, e, i, j, v);
     }
   }
@@ -356,11 +377,14 @@ hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t str
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.splits == 1) return e;
+  const int cols = DIR == kForward ? a.N : a.K;
   const long long rows = DIR == kGradWeights ? (long long)a.E * a.N : a.R;
-  const long long quads = rows * ceil_div(DIR == kForward ? a.N : a.K, 4);
-  hipLaunchKernelGGL((grouped_join_kernel<DIR, I8>),
-                     dim3((unsigned)std::min<long long>((quads + 255) / 256, 4096)), dim3(256), 0,
-                     stream, p);
+  const long long blocks = (rows * ceil_div(cols, 4) + 255) / 256;
+  const dim3 grid((unsigned)std::min<long long>(blocks, 4096)), block(256);
+  if (cols % 4 == 0)
+    hipLaunchKernelGGL((grouped_join_kernel<DIR, I8, true>), grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL((grouped_join_kernel<DIR, I8, false>), grid, block, 0, stream, p);
   return hipGetLastError();
 }
 
