@@ -40,6 +40,7 @@ struct GroupedParams {
   const float* row_scale; // 8-bit integers: of x's rows
   const float* col_scale; // [E,N]
   int splits;             // the sum in this many parts, to `part` if more than one
+  i32x4* row_tiles;       // large tiles: the row tiles of all groups (in the workspace)
   void* part;             // [splits][rows of out][columns] fp32 (8-bit: int32)
 };
 

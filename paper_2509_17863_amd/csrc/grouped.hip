@@ -155,7 +155,7 @@ void grouped_any_kernel(GroupedParams p) {
   constexpr int SUM = 128 / ESZ;  // the sum's elements in a tile
   static_assert(!I8 || DIR == kForward, "8-bit integers: forward only");
   constexpr int kWaves = kThreads / kWave;
-  constexpr int kLds = std::max(2 * kStage, kWaves * kWayOutHalf * 4);
+  constexpr int kLds = std::max(2 * kStage, kWaves * kWayOutBytes);
   __shared__ __attribute__((aligned(16))) char smem[kLds];
   __shared__ int s_find[kThreads / kWave + 4];
   GroupedTile t;
@@ -243,8 +243,8 @@ void grouped_any_kernel(GroupedParams p) {
   }
 
   // (the last barrier is behind every wave's fragment reads)
-  way_out<DIR, I8, 1>(p, t, split, wi, t.j0 + wj, acc,
-                      (LDS_AS float*)smem + wave * kWayOutHalf);
+  way_out<DIR, I8>(p, t, split, wi, t.j0 + wj, acc,
+                   (LDS_AS float*)(smem + wave * kWayOutBytes));
 }
 
 // The parts of a split sum joined, in ascending order: one thread for four
@@ -353,7 +353,9 @@ GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   return g;
 }
 
-size_t part_bytes(const GroupedArgs& a, const GroupedPlan& g) {
+// Workspace: the parts of a split sum, or the large tiles' table of row tiles.
+size_t plan_bytes(const GroupedArgs& a, const GroupedPlan& g) {
+  if (g.kernel == kLarge && a.dir != kGradWeights) return 16 * (1 + most_row_tiles(a, g.bi));
   if (g.splits == 1) return 0;
   const size_t rows = a.dir == kGradWeights ? (size_t)a.E * a.N : (size_t)a.R;
   return (size_t)g.splits * rows * (a.dir == kForward ? a.N : a.K) * 4;
@@ -391,11 +393,11 @@ hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t str
 }  // namespace
 
 size_t grouped_workspace(const GroupedArgs& a) {
-  return part_bytes(a, grouped_plan(a, in_16_bytes(a)));
+  return plan_bytes(a, grouped_plan(a, in_16_bytes(a)));
 }
 
 size_t grouped_workspace_most(const GroupedArgs& a) {
-  return std::max(part_bytes(a, grouped_plan(a, true)), part_bytes(a, grouped_plan(a, false)));
+  return std::max(plan_bytes(a, grouped_plan(a, true)), plan_bytes(a, grouped_plan(a, false)));
 }
 
 hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream) {
@@ -424,6 +426,7 @@ hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream) {
   p.row_scale = a.row_scale;
   p.col_scale = a.col_scale;
   p.part = a.ws;
+  p.row_tiles = static_cast<i32x4*>(a.ws);
   if (a.i8) return launch_product<kForward, true>(p, a, stream);
   if (a.dir == kForward) return launch_product<kForward, false>(p, a, stream);
   if (a.dir == kGradRows) return launch_product<kGradRows, false>(p, a, stream);

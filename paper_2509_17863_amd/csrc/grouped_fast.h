@@ -41,15 +41,14 @@ __device__ __forceinline__ int swz_across(int row) {
 
 // A wave's results, MBW x 2 blocks of 32 x 32, to memory: rows row0.. of the tile,
 // columns col0.. of the result.  They pass through `buf`, kWayOutBytes of LDS that
-// this wave alone uses, 32 rows x 64 columns at a time (in two halves in turn, if
-// there is LDS for both), so that whole row segments are stored.  acc[i][j][v]: row i*32 + lane % 32, column
+// this wave alone uses, 32 rows x 64 columns at a time, so that whole row segments
+// are stored.  acc[i][j][v]: row i*32 + lane % 32, column
 // j*32 + 8*(v/4) + 4*(lane/32) + v % 4.  (A wave's own LDS accesses complete in
 // order.)
 constexpr int kWayOutLd = 68;  // floats: a pad of 16 bytes against bank conflicts
-constexpr int kWayOutHalf = 32 * kWayOutLd;
-constexpr int kWayOutBytes = 2 * kWayOutHalf * 4;
+constexpr int kWayOutBytes = 32 * kWayOutLd * 4;
 
-template <int DIR, bool I8, int HALVES, int MBW, class Acc>
+template <int DIR, bool I8, int MBW, class Acc>
 __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTile& t, int split,
                                         int row0, int col0, const Acc (&acc)[MBW][2],
                                         LDS_AS float* buf) {
@@ -76,7 +75,7 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
       cs[c] = p.col_scale[(size_t)t.e * p.N + min(col + c, p.N - 1)];
   }
   auto stage = [&](int i) {
-    LDS_AS float* at = buf + (i % HALVES) * kWayOutHalf + lrow * LD + 4 * khalf;
+    LDS_AS float* at = buf + lrow * LD + 4 * khalf;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -91,12 +90,10 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
         *reinterpret_cast<LDS_AS f32x4*>(at + j * 32 + 8 * q) = o;
       }
   };
-  if (HALVES == 2) stage(0);
 #pragma unroll
   for (int i = 0; i < MBW; ++i) {
-    if (HALVES == 1) stage(i);
-    else if (i + 1 < MBW) stage(i + 1);
-    const LDS_AS float* from = buf + (i % HALVES) * kWayOutHalf + cl;
+    stage(i);
+    const LDS_AS float* from = buf + cl;
     if (narrow) {
       // 8 lanes to a row of 64 results
 #pragma unroll
