@@ -468,9 +468,9 @@ int eaas_grouped_matmul_dw(const eaas_group_shape *s, const void *dy, int64_t ld
                            const int32_t *offsets, void *dw, int dw_dtype, int accumulate,
                            void *ws, size_t ws_bytes, void *stream);
 
-/* Rows in 8-bit integers, one scale per row: s = amax/127 (1 for a row of
- * zeros), q = x/s to the nearest integer, ties to even, in fp32 arithmetic with
- * correctly rounded quotients.  A row that holds an infinity or a NaN gets a NaN
+/* Rows in 8-bit integers, one scale per row: s = amax * (1/127) with the constant
+ * rounded to fp32 (1 for a row of zeros), q = x/s to the nearest integer, ties to
+ * even; product and quotients in fp32, correctly rounded.  A row that holds an infinity or a NaN gets a NaN
  * scale and zero codes, so whatever is computed from it is NaN.
  *   x [rows,K] bf16 (ldx), q [rows,K] int8 and s [rows] fp32, contiguous
  * Quantizes activations per token, and weights [E,N,K] per output channel

@@ -48,7 +48,7 @@ def grouped_matmul_dw(dy, x, offsets, src):
 
 
 def quantize_rows_int8(x):
-    """(codes, scales) of fp32 rows: scale amax/127 and quotients in fp32, codes
+    """(codes, scales) of fp32 rows: scale amax * fp32(1/127) and quotients in fp32, codes
     to the nearest integer, ties to even; a row that is not finite gets a NaN
     scale and zero codes."""
     x = np.asarray(x, np.float32)
@@ -59,7 +59,7 @@ def quantize_rows_int8(x):
             s[r] = np.nan
             continue
         amax = np.abs(x[r]).max()
-        s[r] = np.float32(1) if amax == 0 else np.float32(amax / np.float32(127))
+        s[r] = np.float32(1) if amax == 0 else np.float32(amax * np.float32(1 / 127))
         q[r] = np.clip(np.rint(x[r] / s[r]), -127, 127).astype(np.int8)
     return q, s
 

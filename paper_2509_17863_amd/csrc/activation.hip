@@ -34,7 +34,8 @@ __device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) 
   if (n >= 8) {
     u32x4 o;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 4; ++i)  // (one instruction a pair)
+      o[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});
     __builtin_memcpy(p, &o, 16);
   } else {
 #pragma unroll
@@ -105,7 +106,9 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const uint16_t* gu, co
 // Rows in 8-bit integers: TPR threads to a row, each with up to HELD chunks of
 // eight values in registers between the row's largest magnitude and its codes
 // (HELD = 0: any length; the values are computed again for the codes).
-// SWIGLU: the values are silu(gate) * up of a row [gate | up] of 2K.
+// SWIGLU: the values are silu(gate) * up of a row [gate | up] of 2K, with the
+// exponential and the quotient of full precision: where a value falls next to the
+// middle between two codes, an error in its last place costs a whole step.
 template <bool SWIGLU, int TPR, int HELD>
 __global__ __launch_bounds__(kThreads) void quantize_int8_kernel(const uint16_t* x, long long ldx,
                                                                  long long rows, int K,
@@ -121,7 +124,7 @@ __global__ __launch_bounds__(kThreads) void quantize_int8_kernel(const uint16_t*
       float up[8];
       load8(row + K + c, K - c, up);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = silu_up(v[i], up[i]);
+      for (int i = 0; i < 8; ++i) v[i] = v[i] / (1.0f + expf(-v[i])) * up[i];
     }
   };
   // magnitudes as integers: NaN above infinity above every finite one
@@ -164,13 +167,29 @@ __global__ __launch_bounds__(kThreads) void quantize_int8_kernel(const uint16_t*
     }
     const bool finite = m < 0x7f800000u;
     const float amax = __uint_as_float(m);
-    const float sc = m == 0 ? 1.0f : finite ? amax / 127.0f : __uint_as_float(0x7fc00000u);
+    const float sc = m == 0 ? 1.0f : finite ? amax * (1.0f / 127.0f) : __uint_as_float(0x7fc00000u);
+    const float inv = __builtin_amdgcn_rcpf(sc);
     auto emit = [&](int ch, const float (&v)[8]) {
+      // A product with the reciprocal is within 1e-4 of the quotient (at most 128, a
+      // few units in the last place): it gives the same code unless that close to
+      // the middle between two (or not a number: a scale below the normal range),
+      // where the quotient itself decides.
+      float t[8];
+      bool close = false;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        t[i] = v[i] * inv;
+        close |= !(fabsf(t[i] - rintf(t[i])) < 0.4999f);
+      }
+      if (close) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = v[i] / sc;
+      }
       uint32_t w[2] = {0, 0};
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         // (a scale below the normal range is coarse: keep its quotients in range)
-        const int code = finite ? (int)fminf(fmaxf(rintf(v[i] / sc), -127.0f), 127.0f) : 0;
+        const int code = finite ? (int)fminf(fmaxf(rintf(t[i]), -127.0f), 127.0f) : 0;
         w[i / 4] |= (uint32_t)(code & 0xff) << (8 * (i % 4));
       }
       int8_t* o = q + r * K + ch * 8;

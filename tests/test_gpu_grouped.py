@@ -120,8 +120,20 @@ SHAPES = [
 ]
 
 
+# groups of many rows and matrices large enough for the 256 x 256 tiles (forward,
+# gradient in the rows: N resp. K wide; gradient in the weights: both), rows and
+# columns that end inside one, sums that end inside a step, more tiles than CUs
+LARGE = [
+    (1500, 3, 6200, 72, "ragged", 0, 0),
+    (1040, 2, 9000, 136, "even", 4, 8),
+    (1024, 4, 200, 9224, "some", 0, 0),
+    (1030, 5, 1800, 1544, "even", 0, 0),
+    (1290, 3, 2568, 2056, "ragged", 6, 8),
+]
+
+
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
-@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
 def test_forward(gpu, shape, out):
     c = Case(*shape)
     y = c.out(c.R, c.N, out)
@@ -131,7 +143,7 @@ def test_forward(gpu, shape, out):
 
 
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
-@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
 def test_gradient_in_the_rows(gpu, shape, out):
     c = Case(*shape)
     dx = c.out(c.R, c.K, out)
@@ -141,7 +153,7 @@ def test_gradient_in_the_rows(gpu, shape, out):
 
 
 @pytest.mark.parametrize("mode", ["bf16", "fp32", "accumulate"])
-@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
 def test_gradient_in_the_weights(gpu, shape, mode):
     c = Case(*shape)
     dt = torch.bfloat16 if mode == "bf16" else torch.float32
@@ -161,7 +173,7 @@ def test_gradient_in_the_weights(gpu, shape, mode):
 
 
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
-@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
 def test_int8(gpu, shape, out):
     c = Case(*shape, i8=True)
     y = c.out(c.R, c.N, out)
