@@ -225,9 +225,17 @@ hipError_t launch_int8(const uint16_t* x, long long ldx, long long rows, int K,
                        dim3(kThreads), 0, stream, x, ldx, rows, K, n_rows, q, s);
     return hipGetLastError();
   };
-  if (K <= 512) return go(quantize_int8_kernel<SWIGLU, 64, 1>, 64);
+  // A wave to a row where there are rows enough to fill the chip with them (no
+  // barrier, and a lane's chunks are loaded together): 32768 rows of 2048 in 89 us
+  // against 110 with a workgroup to a row; else a workgroup to a row.
+  if (rows >= 2048 && K <= 2048) {
+    if (K <= 512) return go(quantize_int8_kernel<SWIGLU, 64, 1>, 64);
+    if (K <= 1024) return go(quantize_int8_kernel<SWIGLU, 64, 2>, 64);
+    return go(quantize_int8_kernel<SWIGLU, 64, 4>, 64);
+  }
   if (K <= 2048) return go(quantize_int8_kernel<SWIGLU, 256, 1>, 256);
   if (K <= 8192) return go(quantize_int8_kernel<SWIGLU, 256, 4>, 256);
+  if (K <= 16384) return go(quantize_int8_kernel<SWIGLU, 256, 8>, 256);
   return go(quantize_int8_kernel<SWIGLU, 256, 0>, 256);
 }
 

@@ -339,18 +339,34 @@ int sum_parts(const GroupedArgs& a, long long tiles, int enough, int least) {
   return (int)std::max<long long>(1, std::min<long long>(enough / tiles, steps / least));
 }
 
+// The choice, with both sides measured (us, rows of each group x E groups, N x K).
+//   Large tiles on every CU, groups of some rows (they read the weights as fast as
+//   the few-rows kernel, and each byte once): dx 24 x 32, 4096 x 7168: 362 large, 370
+//   few; 16 x 128, 1536 x 2048: 151, 175; 8-bit 24 x 32: 172, 187; forward 64 x 32:
+//   346, 373, but 32 x 128: 195, 182.  dW 128 x 32, 2048 x 2048: 100 large, 131 any;
+//   64 x 128, 1536 x 2048: 274, 270.
+//   Few rows, or few tiles: 64 x 8, 4096 x 4096, forward: 49 few, 77 any, 74 large;
+//   512 x 1: 33, 42, 68; 256 x 8, 1024 x 1024, dx: 17, 36, 25.
+//   Between them the tiles of any alignment (512 x 8, 1024 x 1024, forward: 20 any,
+//   25 large, 31 few), except dx over a long sum, where the rows of W that a tile
+//   takes lie on few memory channels: 1024 x 8, 1024 x 1024: 28 large, 38 any; but
+//   2048 x 8, 256 x 136: 19, 12.  dW on fewer large tiles than CUs: 4096 x 1, 1024 x
+//   4096 (64 tiles): 78 large, 180 any; 4096 x 8, 256 x 256 (8 tiles): 74, 29.
 GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   const long long rows = a.R / std::max(1, std::min(a.R, a.E));  // of a group that has any
-  if (in16 && a.dir != kGradWeights && rows <= 64) {
+  const long long tiles = out_tiles(a, kBI, kBJ), large = out_tiles(a, 256, 256);
+  const GroupedPlan on_large{kLarge, 256, 256, 1};
+  const GroupedPlan any{kAny, kBI, kBJ, sum_parts(a, tiles, 512, 8)};
+  if (!in16) return any;
+  if (a.dir == kGradWeights) return rows >= 128 && large >= 48 ? on_large : any;
+  const int some = a.dir == kForward && !a.i8 ? 48 : 16;
+  if (rows >= some && large >= 192) return on_large;
+  if (rows <= 64 || tiles <= 192) {
     GroupedPlan g{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};
     g.splits = sum_parts(a, out_tiles(a, g.bi, g.bj), 512, 8);
     return g;
   }
-  const long long tiles = out_tiles(a, kBI, kBJ);
-  GroupedPlan g{kAny, kBI, kBJ, sum_parts(a, tiles, 512, 8)};
-  if (in16 && g.splits == 1 && rows >= 128 && out_tiles(a, 256, 256) >= 192)
-    g = GroupedPlan{kLarge, 256, 256, 1};
-  return g;
+  return a.dir == kGradRows && large >= 80 && a.N >= 512 ? on_large : any;
 }
 
 // Workspace: the parts of a split sum, or the large tiles' table of row tiles.

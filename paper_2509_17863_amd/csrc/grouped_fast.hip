@@ -86,7 +86,8 @@ __global__ __launch_bounds__(1024) void row_tiles_kernel(GroupedParams p) {
   s_before[tid] = incl - mine;
   if (tid == 1023) s_before[1024] = incl;
   __syncthreads();
-  const int total = s_before[1024];
+  // (offsets that do not ascend can name more tiles than the table holds)
+  const int total = min(s_before[1024], p.R / kB + min(p.R, p.E));
   if (tid == 0) p.row_tiles[0] = i32x4{total, 0, 0, 0};
   for (int n = tid; n < total; n += 1024) {
     // the last group whose tiles start at or before n (groups without rows share

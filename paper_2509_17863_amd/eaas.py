@@ -182,7 +182,8 @@ def _p(t):
 
 def _stream(stream):
     if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+        # (the handle alone: a torch Stream object costs 2.6 us more, a third of a small call)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -237,6 +237,23 @@ def test_offsets_outside_the_rows_are_clamped(gpu):
     c.check(y, want, mag, c.K)
 
 
+@pytest.mark.parametrize("R,E,N,K", [(1024, 8, 6200, 72), (64, 8, 64, 2048), (300, 6, 33, 47)])
+def test_offsets_that_do_not_ascend_stay_in_bounds(gpu, R, E, N, K):
+    """Results are then undefined, but nothing outside the result is written."""
+    c = Case(R, E, N, K, "even")
+    wild = torch.tensor([0, R] * (E // 2) + [0], dtype=torch.int32, device="cuda")
+    guard = torch.zeros(c.ws.numel() + 4096, dtype=torch.uint8, device="cuda")
+    ws = guard[: c.ws.numel()]
+    y, dx = c.out(R + 8, N, torch.float32), c.out(R + 8, K, torch.float32)
+    dw = torch.full((E + 1, N, K), CANARY, device="cuda")
+    eaas.eaas_grouped_matmul(c.dx_, wild, c.dw_, y[:R], ws)
+    eaas.eaas_grouped_matmul_dx(c.ddy, wild, c.dw_, dx[:R], ws)
+    eaas.eaas_grouped_matmul_dw(c.ddy, c.dx_, wild, dw[:E], ws)
+    torch.cuda.synchronize()
+    assert (y[R:] == CANARY).all() and (dx[R:] == CANARY).all() and (dw[E] == CANARY).all()
+    assert (guard[c.ws.numel():] == 0).all()
+
+
 def test_another_stream_and_a_graph(gpu):
     c = Case(512, 4, 128, 256, "even", k=2)
     y = c.out(c.R, c.N, torch.float32)
