@@ -514,8 +514,9 @@ void grouped_pp_kernel(GroupedParams p) {
     const bool live = grp * 128 < t.i_valid && t.j0 + w4 * 64 < cols;
     if (nk > 0) {
       phase_end();
-      // both groups pass 2*nk + 1 barriers: group 1 idles in the first phase, group
-      // 0 in the last.  Tiles 0 and 1 have landed: the waits start with tile 2.
+      // both groups pass 2*nk barriers: group 1 idles in the first phase, and group
+      // 0 goes on to the next results while group 1 has its last MFMAs to issue.
+      // Tiles 0 and 1 have landed: the waits start with tile 2.
       if (grp == 0) {
 #pragma unroll 1
         for (int kt = 0; kt < nk; ++kt) {
@@ -527,7 +528,6 @@ void grouped_pp_kernel(GroupedParams p) {
           if (kt >= 1) wait_vmcnt<0>();
           phase_end();
         }
-        phase_end();
       } else {
         phase_end();
 #pragma unroll 1
@@ -541,7 +541,7 @@ void grouped_pp_kernel(GroupedParams p) {
           }
           phase_end();
           mfmas(f);
-          phase_end();
+          if (kt + 1 < nk) phase_end();
         }
       }
     }
