@@ -56,8 +56,8 @@ __device__ __forceinline__ GroupedParams fresh_params() {
 }
 // A scalar that the compiler takes for a new one here, so that what is computed
 // from it is computed again instead of being held across the main loop.
-template <class T>
-__device__ __forceinline__ T opaque(T v) {
+__device__ __forceinline__ uint32_t opaque(uint32_t v) {
+  v = __builtin_amdgcn_readfirstlane(v);
   asm volatile("" : "+s"(v));
   return v;
 }
@@ -353,9 +353,9 @@ void grouped_pp_kernel(GroupedParams p) {
       load_lds16(d, in ? along_off[q % kOffs] + (kOffs == 1 ? q * step : 0) : kNowhere,
                  lds + (w4 + 4 * q) * 1024);
   };
-  auto issue_across = [&](int kt, uint32_t lds, long long row, int width) INLINE {
+  auto issue_across = [&](int kt, uint32_t lds, long long row_bytes, int width) INLINE {
     lds = opaque(lds);
-    row = opaque(row);
+    const long long row = opaque((uint32_t)row_bytes);
     const int left = min(64, sum_end - kt * 64);
     const i32x4 d = descriptor(across_base + (long long)kt * 64 * row,
                                (uint32_t)((left - 1) * row + (long long)width * ESZ));
@@ -450,7 +450,8 @@ void grouped_pp_kernel(GroupedParams p) {
       return *reinterpret_cast<const LDS_AS u32x4*>(stage + (at ^ (kk << 5)) + block * 4096);
     }
   };
-  auto load_frags = [&](int kt, Frags& f) INLINE {
+  // mb: row blocks of this wave that hold rows of the result
+  auto load_frags = [&](auto mb, int kt, Frags& f) INLINE {
     const LDS_AS char* sa = smem + (kt % kSA) * kStage;
     const LDS_AS char* sb = smem + (kSA + kt % kSB) * kStage;
     int a0 = a_at, b0 = b_at;
@@ -461,18 +462,18 @@ void grouped_pp_kernel(GroupedParams p) {
       for (int j = 0; j < NBW; ++j)
         f.b[kk][j] = fragment(std::integral_constant<bool, B_ACROSS>{}, sb, b0, j, kk);
 #pragma unroll
-      for (int i = 0; i < MBW; ++i)
+      for (int i = 0; i < decltype(mb)::value; ++i)
         f.a[kk][i] = fragment(std::integral_constant<bool, A_ACROSS>{}, sa, a0, i, kk);
     }
     // the stage may be filled again right after the next barrier
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   };
-  auto mfmas = [&](const Frags& f) INLINE {
+  auto mfmas = [&](auto mb, const Frags& f) INLINE {
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-      for (int i = 0; i < MBW; ++i)
+      for (int i = 0; i < decltype(mb)::value; ++i)
 #pragma unroll
         for (int j = 0; j < NBW; ++j) {
           if constexpr (I8)
@@ -500,6 +501,39 @@ void grouped_pp_kernel(GroupedParams p) {
     issue(0);
     if (nk > 1) issue(1);
   };
+  // The sum of one tile of results.  Both groups pass 2*nk barriers: group 1 idles in
+  // the first phase, and group 0 goes on to the next results while group 1 has its
+  // last MFMAs to issue.  Tiles 0 and 1 have landed: the waits start with tile 2.
+  auto walk = [&](auto mb) INLINE {
+    constexpr bool LIVE = decltype(mb)::value > 0;
+    if (grp == 0) {
+#pragma unroll 1
+      for (int kt = 0; kt < nk; ++kt) {
+        if (kt >= 1 && kt + 1 < nk) issue(kt + 1);
+        Frags f;
+        if constexpr (LIVE) load_frags(mb, kt, f);
+        phase_end();
+        if constexpr (LIVE) mfmas(mb, f);
+        if (kt >= 1) wait_vmcnt<0>();
+        phase_end();
+      }
+    } else {
+      phase_end();
+#pragma unroll 1
+      for (int kt = 0; kt < nk; ++kt) {
+        if (kt + 2 < nk) issue(kt + 2);
+        Frags f;
+        if constexpr (LIVE) load_frags(mb, kt, f);
+        if (kt >= 1) {
+          if (kt + 2 < nk) wait_vmcnt<kInst>();
+          else wait_vmcnt<0>();
+        }
+        phase_end();
+        if constexpr (LIVE) mfmas(mb, f);
+        if (kt + 1 < nk) phase_end();
+      }
+    }
+  };
   int id = blockIdx.x;
   if (id >= total) return;
   locate(id);
@@ -510,40 +544,14 @@ void grouped_pp_kernel(GroupedParams p) {
     for (int i = 0; i < MBW; ++i)
 #pragma unroll
       for (int j = 0; j < NBW; ++j) acc[i][j] = Acc{};
-    // (a wave without results here keeps loading for the others)
-    const bool live = grp * 128 < t.i_valid && t.j0 + w4 * 64 < cols;
     if (nk > 0) {
       phase_end();
-      // both groups pass 2*nk barriers: group 1 idles in the first phase, and group
-      // 0 goes on to the next results while group 1 has its last MFMAs to issue.
-      // Tiles 0 and 1 have landed: the waits start with tile 2.
-      if (grp == 0) {
-#pragma unroll 1
-        for (int kt = 0; kt < nk; ++kt) {
-          if (kt >= 1 && kt + 1 < nk) issue(kt + 1);
-          Frags f;
-          load_frags(kt, f);
-          phase_end();
-          mfmas(f);
-          if (kt >= 1) wait_vmcnt<0>();
-          phase_end();
-        }
-      } else {
-        phase_end();
-#pragma unroll 1
-        for (int kt = 0; kt < nk; ++kt) {
-          if (kt + 2 < nk) issue(kt + 2);
-          Frags f;
-          load_frags(kt, f);
-          if (kt >= 1) {
-            if (kt + 2 < nk) wait_vmcnt<kInst>();
-            else wait_vmcnt<0>();
-          }
-          phase_end();
-          mfmas(f);
-          if (kt + 1 < nk) phase_end();
-        }
-      }
+      // a wave multiplies the row blocks that exist (rounded up to 0, 2 or 4), and
+      // loads its share for the others in any case
+      const int rows = t.j0 + w4 * 64 < cols ? t.i_valid - grp * 128 : 0;
+      if (rows > 64) walk(std::integral_constant<int, 4>{});
+      else if (rows > 0) walk(std::integral_constant<int, 2>{});
+      else walk(std::integral_constant<int, 0>{});
     }
     // The next results' operands go ahead of the stores (the last barrier is behind
     // every wave's fragment reads; the stores pass through B's third stage), and
