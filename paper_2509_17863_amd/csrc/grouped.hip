@@ -72,37 +72,27 @@ struct Loader {
       for (int q = 0; q < 4; ++q) row[q] = rp(q, r0 + 32 * q);
     }
   }
-  // s0: the sum's index where the tile starts; s_end: where the sum ends
+  // s0: the sum's index where the tile starts; s_end: where the sum ends.  (One
+  // branch around all of a tile's loads: with one around each they were waited for
+  // one by one, 8 round trips a tile.)
   template <class RowPtr>
   __device__ __forceinline__ void load(RowPtr rp, int s0, int s_end, int c0, int width) {
-    if constexpr (ACROSS) {
-      const int c = c0 + chunk * EPC;
-      const bool inside = s0 + 64 <= s_end && c0 + 128 <= width;
+    const int c = ACROSS ? c0 + chunk * EPC : 0, s_first = ACROSS ? s0 + r0 : s0 + chunk * EPC;
+    auto at = [&](int q) {
+      return ACROSS ? rp(q, s_first + 16 * q) + (size_t)c * ESZ
+                    : row[ACROSS ? 0 : q] + (size_t)s_first * ESZ;
+    };
+    const bool inside = ACROSS ? s0 + 64 <= s_end && c0 + 128 <= width : s0 + 8 * EPC <= s_end;
+    if (__builtin_amdgcn_readfirstlane(inside)) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int s = s0 + r0 + 16 * q;
-        if (inside) {
-          v[q] = load16(rp(q, s) + (size_t)c * ESZ);
-        } else {
-          v[q] = u32x4{0, 0, 0, 0};
-          if (s < s_end && c < width) {
-            const char* p = rp(q, s) + (size_t)c * ESZ;
-            v[q] = c + EPC <= width ? load16(p) : load_some<ESZ>(p, width - c);
-          }
-        }
-      }
+      for (int q = 0; q < 4; ++q) v[q] = load16(at(q));
     } else {
-      const int s = s0 + chunk * EPC;
-      const bool inside = s0 + 8 * EPC <= s_end;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const char* p = row[q] + (size_t)s * ESZ;
-        if (inside) {
-          v[q] = load16(p);
-        } else {
-          v[q] = u32x4{0, 0, 0, 0};
-          if (s < s_end) v[q] = s + EPC <= s_end ? load16(p) : load_some<ESZ>(p, s_end - s);
-        }
+        v[q] = u32x4{0, 0, 0, 0};
+        const int n = ACROSS ? (s_first + 16 * q < s_end ? width - c : 0) : s_end - s_first;
+        if (n >= EPC) v[q] = load16(at(q));
+        else if (n > 0) v[q] = load_some<ESZ>(at(q), n);
       }
     }
   }
