@@ -13,6 +13,11 @@
 // and read back 16 bytes a lane; one that lies across it is kept as it comes, 64
 // rows of 128 columns, and read with the transposing LDS load, which hands each
 // lane four elements of its column.
+//
+// What bounds it: loads that straddle lines (a wave's 16-byte loads take 7.6 ns on
+// aligned rows, 13.8 where rows start on any dword, 27 on any 2 bytes), then LDS.
+// 8 experts of 1024 rows, 4097 x 8191: forward 0.91 ms (603 TFLOP/s), dx 0.96, dW
+// 0.96; 8-bit integers 0.56 (981 TOP/s).
 #include <algorithm>
 
 #include "grouped_fast.h"

@@ -8,8 +8,14 @@
 // barriers: it loads tiles of 128 bytes of the sum (64 bf16, 128 8-bit values) of
 // its 64 weight rows (kGradRows: 64 rows of the sum x 64 columns) and of the rows,
 // 8 + 2 * MB KiB, straight into its own two LDS stages, whole 128-byte lines at a
-// time, and refills a stage as soon as it has read it.  Two workgroups to a CU keep
-// about 128 KiB in flight there, several times what the memory's latency asks for.
+// time, and refills a stage as soon as it has read it.  (Two stages and two workgroups
+// to a CU for 16 rows; three stages for 32 and two for 64, one workgroup: 96 to 150
+// KiB in flight on a CU, several times what the memory's latency asks for.)
+//
+// Measured, reading the weights once: 4 rows of each of 128 experts, 2048 x 768:
+// forward 77 us (5.2 TB/s), dx 72 (5.6); one token, 8 of 32
+// experts, 4096 x 7168 in 8-bit integers: 41 us (5.7); 32 rows of each of 32 experts,
+// 4096 x 7168, bf16: 333 (5.7).
 #include "grouped_fast.h"
 
 namespace eaas {
