@@ -325,43 +325,84 @@ struct GroupedPlan {
   int splits;
 };
 
-// Parts of the sum: where the tiles leave most of the chip idle, as many as make
-// `enough` workgroups, of at least `least` tiles of the sum each.
-int sum_parts(const GroupedArgs& a, long long tiles, int enough, int least) {
-  const int sum = a.dir == kForward ? a.K : a.dir == kGradRows ? a.N : a.R;
-  const int steps = ceil_div(sum, a.i8 ? 128 : 64);
-  if (tiles <= 0 || tiles * 8 >= 3 * enough) return 1;
-  return (int)std::max<long long>(1, std::min<long long>(enough / tiles, steps / least));
+// The time of a product on one kernel in us, which the choice below compares: a
+// fixed part, what a tile's steps of the sum (64, or 128 in 8 bits) take on a CU of
+// its own, and how workgroups that share a CU slow one another (three of the any
+// kernel's fit, of which 0.65 of a step each comes out).  Splitting a sum adds a
+// launch that joins its parts.  The constants are fitted to 88 of 254 shapes (groups
+// of 1 to 4000 rows, 1 to 63 groups, N and K of 64 to 13000) x 4 products x up to 13
+// ways of computing each, all timed: 10% off on average, and over all shapes what
+// they choose takes 2% longer than the fastest way (thresholds on sizes alone: 10%
+// forward, 9% 8-bit, 7% dx, 4% dW).
+constexpr int kCUs = 256;
+
+double join_us(double out, int splits) { return splits == 1 ? 0 : 3.5 + 1.4e-6 * out * splits; }
+
+double any_us(double tiles, int steps, int splits) {
+  return 6 + std::max(1.0, 0.65 * tiles * splits / kCUs) * ceil_div(steps, splits);
 }
 
-// The choice, with both sides measured (us, rows of each group x E groups, N x K).
-//   Large tiles on every CU, groups of some rows (they read the weights as fast as
-//   the few-rows kernel, and each byte once): dx 24 x 32, 4096 x 7168: 362 large, 370
-//   few; 16 x 128, 1536 x 2048: 151, 175; 8-bit 24 x 32: 172, 187; forward 64 x 32:
-//   346, 373, but 32 x 128: 195, 182.  dW 128 x 32, 2048 x 2048: 100 large, 131 any;
-//   64 x 128, 1536 x 2048: 274, 270.
-//   Few rows, or few tiles: 64 x 8, 4096 x 4096, forward: 49 few, 77 any, 74 large;
-//   512 x 1: 33, 42, 68; 256 x 8, 1024 x 1024, dx: 17, 36, 25.
-//   Between them the tiles of any alignment (512 x 8, 1024 x 1024, forward: 20 any,
-//   25 large, 31 few), except dx over a long sum, where the rows of W that a tile
-//   takes lie on few memory channels: 1024 x 8, 1024 x 1024: 28 large, 38 any; but
-//   2048 x 8, 256 x 136: 19, 12.  dW on fewer large tiles than CUs: 4096 x 1, 1024 x
-//   4096 (64 tiles): 78 large, 180 any; 4096 x 8, 256 x 256 (8 tiles): 74, 29.
+double few_us(double tiles, int steps, int bi, int splits) {  // 4 waves share the steps
+  return 5 + std::max(1.0, 1.25 * tiles * splits / kCUs) *
+                 (3 + (bi == 64 ? 0.6 : 0.4) * ceil_div(ceil_div(steps, splits), 4));
+}
+
+double large_us(double tiles, int steps) {
+  return std::max(1.0, tiles / kCUs) * (10 + 0.92 * steps);
+}
+
+// Parts of the sum: the fewest that the estimate finds best.
+template <typename F>
+int best_parts(int steps, double out, F&& us, double* time) {
+  int best = 1;
+  *time = us(1);
+  for (int s = 2; s <= steps && s <= 2 * kCUs; s += 1 + s / 8) {
+    const double t = us(s) + join_us(out, s);
+    if (t < *time) *time = t, best = s;
+  }
+  return best;
+}
+
+// The choice.  Two regions are taken before the estimates, which know no memory
+// traffic; both sides measured (us, rows of each group x E groups, N x K):
+//   Large tiles on every CU, groups of some rows and a sum of some steps: they read
+//   the weights as fast as the few-rows kernel, and each byte once.  dx 24 x 32, 4096
+//   x 7168: 362 large, 370 few; 16 x 128, 1536 x 2048: 151, 175; 8-bit 24 x 32: 172,
+//   187; forward 64 x 32: 346, 373, but 32 x 128: 195, 182.  2500 x 16, 4096 x 512
+//   (8 steps): 123 large, 174 any; but 482 x 19, 2208 x 160 (3 steps): 33, 23.
+//   dW 128 x 32, 2048 x 2048: 100 large, 131 any; 64 x 128, 1536 x 2048: 274, 270;
+//   on fewer large tiles than CUs 4096 x 1, 1024 x 4096 (64 tiles): 78 large, 180 any;
+//   4096 x 8, 256 x 256 (8 tiles): 74, 29.
+//   Groups of one to 24 rows, a sum of some steps: tiles of 16 or 32 rows, which the
+//   others would leave mostly empty.  20 x 8, 4096 x 4096, forward: 45 few, 52 any in 3 parts,
+//   63 large; 14 x 53, 160 x 3600, dx (3 steps): 50 few, 24 any.
+// What the estimates decide: forward 200 x 1, 1024 x 1024: 9 few in one part, 12 in
+// 4; 215 x 3, 464 x 12176: 35 any in 16 parts, 45 few in 4; 2500 x 4, 512 x 8192:
+// 128 large, 137 any in 2 parts, 139 few.
 GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   const long long rows = a.R / std::max(1, std::min(a.R, a.E));  // of a group that has any
-  const long long tiles = out_tiles(a, kBI, kBJ), large = out_tiles(a, 256, 256);
+  const long long sum = a.dir == kForward ? a.K : a.dir == kGradRows ? a.N : rows;
+  const int steps = ceil_div((int)sum, a.i8 ? 128 : 64);
+  const double out = a.dir == kGradWeights ? (double)a.E * a.N * a.K
+                                           : (double)a.R * (a.dir == kForward ? a.N : a.K);
+  const double tiles = (double)out_tiles(a, kBI, kBJ);
+  const long long large = out_tiles(a, 256, 256);
   const GroupedPlan on_large{kLarge, 256, 256, 1};
-  const GroupedPlan any{kAny, kBI, kBJ, sum_parts(a, tiles, 512, 8)};
+  GroupedPlan any{kAny, kBI, kBJ, 1};
+  double t_any;
+  any.splits = best_parts(steps, out, [&](int s) { return any_us(tiles, steps, s); }, &t_any);
   if (!in16) return any;
   if (a.dir == kGradWeights) return rows >= 128 && large >= 48 ? on_large : any;
   const int some = a.dir == kForward && !a.i8 ? 48 : 16;
-  if (rows >= some && large >= 192) return on_large;
-  if (rows <= 64 || tiles <= 192) {
-    GroupedPlan g{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};
-    g.splits = sum_parts(a, out_tiles(a, g.bi, g.bj), 512, 8);
-    return g;
-  }
-  return a.dir == kGradRows && large >= 80 && a.N >= 512 ? on_large : any;
+  if (rows >= some && large >= 192 && steps >= 4) return on_large;
+  GroupedPlan few{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};
+  const double cells = (double)out_tiles(a, few.bi, few.bj);
+  double t_few;
+  few.splits = best_parts(steps, out, [&](int s) { return few_us(cells, steps, few.bi, s); },
+                          &t_few);
+  if (rows <= 24 && steps >= 4) return few;
+  const double t_large = large_us((double)large, steps);
+  return t_large < std::min(t_any, t_few) ? on_large : t_few < t_any ? few : any;
 }
 
 // Workspace: the parts of a split sum, or the large tiles' table of row tiles.
