@@ -16,8 +16,8 @@
 //
 // What bounds it: loads that straddle lines (a wave's 16-byte loads take 7.6 ns on
 // aligned rows, 13.8 where rows start on any dword, 27 on any 2 bytes), then LDS.
-// 8 experts of 1024 rows, 4097 x 8191: forward 0.91 ms (603 TFLOP/s), dx 0.96, dW
-// 0.96; 8-bit integers 0.56 (981 TOP/s).
+// 8 experts of 1024 rows, 4097 x 8191: forward 0.85 ms (648 TFLOP/s), dx 0.92, dW
+// 0.95; 8-bit integers 0.54 (1019 TOP/s).
 #include <algorithm>
 
 #include "grouped_fast.h"
