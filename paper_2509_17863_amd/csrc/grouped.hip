@@ -336,7 +336,9 @@ struct GroupedPlan {
 // forward, 9% 8-bit, 7% dx, 4% dW).
 constexpr int kCUs = 256;
 
-double join_us(double out, int splits) { return splits == 1 ? 0 : 3.5 + 1.4e-6 * out * splits; }
+double join_us(double out, int splits) {  // (a thread's loads of its parts are a chain)
+  return splits == 1 ? 0 : 3.5 + (0.06 + 1.4e-6 * out) * splits;
+}
 
 double any_us(double tiles, int steps, int splits) {
   return 6 + std::max(1.0, 0.65 * tiles * splits / kCUs) * ceil_div(steps, splits);

@@ -132,8 +132,22 @@ LARGE = [
 ]
 
 
+# the large tiles again where the sum is of some steps, in every direction (8-bit
+# included) and with empty groups; and sums of one to many parts
+LONGER = [
+    (1200, 4, 8200, 464, "some", 0, 0),
+    (1040, 2, 9000, 528, "even", 4, 8),
+    (1024, 4, 264, 9224, "ragged", 0, 0),
+    (5, 1, 40, 70000, "one", 0, 0),
+    (9, 2, 33, 30001, "even", 3, 1),
+    (3, 2, 30000, 48, "some", 0, 0),
+    (30000, 1, 24, 40, "even", 2, 0),
+    (200, 2, 264, 9000, "one", 4, 8),
+]
+
+
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
-@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE + LONGER, ids=str)
 def test_forward(gpu, shape, out):
     c = Case(*shape)
     y = c.out(c.R, c.N, out)
@@ -143,7 +157,7 @@ def test_forward(gpu, shape, out):
 
 
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
-@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE + LONGER, ids=str)
 def test_gradient_in_the_rows(gpu, shape, out):
     c = Case(*shape)
     dx = c.out(c.R, c.K, out)
@@ -153,7 +167,7 @@ def test_gradient_in_the_rows(gpu, shape, out):
 
 
 @pytest.mark.parametrize("mode", ["bf16", "fp32", "accumulate"])
-@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE + LONGER, ids=str)
 def test_gradient_in_the_weights(gpu, shape, mode):
     c = Case(*shape)
     dt = torch.bfloat16 if mode == "bf16" else torch.float32
@@ -173,7 +187,7 @@ def test_gradient_in_the_weights(gpu, shape, mode):
 
 
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
-@pytest.mark.parametrize("shape", SHAPES + LARGE, ids=str)
+@pytest.mark.parametrize("shape", SHAPES + LARGE + LONGER, ids=str)
 def test_int8(gpu, shape, out):
     c = Case(*shape, i8=True)
     y = c.out(c.R, c.N, out)
