@@ -551,6 +551,10 @@ void grouped_pp_kernel(GroupedParams p) {
 #pragma unroll
       for (int j = 0; j < NBW; ++j) acc[i][j] = Acc{};
     if (nk > 0) {
+      // The stores' passes through B's third stage end here: a wave whose rows do not
+      // all exist need not have waited for its last ones, and group 1 loads into that
+      // stage two barriers from here.
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       phase_end();
       // a wave multiplies the row blocks that exist (rounded up to 0, 2 or 4), and
       // loads its share for the others in any case
