@@ -67,14 +67,23 @@ __device__ __forceinline__ float silu_up(float g, float up) {
   return (g * t.hi) * t.lo * up;
 }
 
-// g / (1 + exp(-g)) to within half a unit in the last place, or rarely a little more:
-// the full exponential, and a quotient corrected by its remainder.
+// g / (1 + exp(-g)) from a gate of kFar or more, to about two units in the last place:
+// the full exponential and its sum with 1 are rounded, the quotient is corrected by
+// its remainder.  (The reciprocal is a normal number there.)
+constexpr float kFar = -86.0f;
 __device__ __forceinline__ float silu_full(float g) {
   const float d = 1.0f + expf(-g);
   const float y = __builtin_amdgcn_rcpf(d);
   const float q = g * y;
-  const float c = fmaf(fmaf(-q, d, g), y, q);
-  return d < 3e38f ? c : g * 0.0f;
+  return fmaf(fmaf(-q, d, g), y, q);
+}
+
+// The same times up, below kFar: the quotient is g exp(g) to fp32, whose exponential
+// leaves the normal range from -87.3 on; two factors exp(g / 2) do not, and each takes
+// its share of the product.
+__device__ __forceinline__ float silu_far_up(float g, float up) {
+  const float z = expf(0.5f * g);
+  return (g * z) * (z * up);
 }
 
 __device__ __forceinline__ long long live_rows(long long rows, const int32_t* n_rows) {
@@ -134,10 +143,21 @@ __global__ __launch_bounds__(kThreads) void quantize_int8_kernel(const uint16_t*
   auto value = [&](const uint16_t* row, int c, float (&v)[8]) {
     load8(row + c, K - c, v);
     if constexpr (SWIGLU) {
-      float up[8];
+      float up[8], o[8];
       load8(row + K + c, K - c, up);
+      bool far = false;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = silu_full(v[i]) * up[i];
+      for (int i = 0; i < 8; ++i) {
+        o[i] = silu_full(v[i]) * up[i];
+        far |= v[i] < kFar;
+      }
+      if (far) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (v[i] < kFar) o[i] = silu_far_up(v[i], up[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = o[i];
     }
   };
   // magnitudes as integers: NaN above infinity above every finite one
