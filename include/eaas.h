@@ -469,9 +469,10 @@ int eaas_grouped_matmul_dw(const eaas_group_shape *s, const void *dy, int64_t ld
                            void *ws, size_t ws_bytes, void *stream);
 
 /* Rows in 8-bit integers, one scale per row: s = amax * (1/127) with the constant
- * rounded to fp32 (1 for a row of zeros), q = x/s to the nearest integer, ties to
- * even; product and quotients in fp32, correctly rounded.  A row that holds an infinity or a NaN gets a NaN
- * scale and zero codes, so whatever is computed from it is NaN.
+ * rounded to fp32 (1 where that is zero: rows of zeros, or below 2^-143), q = x/s to
+ * the nearest integer, ties to even; product and quotients in fp32, correctly rounded.
+ * A row that holds an infinity or a NaN gets a NaN scale and zero codes, so whatever is
+ * computed from it is NaN.
  *   x [rows,K] bf16 (ldx), q [rows,K] int8 and s [rows] fp32, contiguous
  * Quantizes activations per token, and weights [E,N,K] per output channel
  * (rows = E*N).  rows = 0: nothing.  Errors: INVALID_ARG, UNSUPPORTED (rows or K

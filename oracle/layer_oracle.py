@@ -48,9 +48,9 @@ def grouped_matmul_dw(dy, x, offsets, src):
 
 
 def quantize_rows_int8(x):
-    """(codes, scales) of fp32 rows: scale amax * fp32(1/127) and quotients in fp32, codes
-    to the nearest integer, ties to even; a row that is not finite gets a NaN
-    scale and zero codes."""
+    """(codes, scales) of fp32 rows: scale amax * fp32(1/127), 1 where that is zero, and
+    quotients in fp32, codes to the nearest integer, ties to even; a row that is not
+    finite gets a NaN scale and zero codes."""
     x = np.asarray(x, np.float32)
     q = np.zeros(x.shape, np.int8)
     s = np.zeros(x.shape[0], np.float32)
@@ -58,8 +58,8 @@ def quantize_rows_int8(x):
         if not np.isfinite(x[r]).all():
             s[r] = np.nan
             continue
-        amax = np.abs(x[r]).max()
-        s[r] = np.float32(1) if amax == 0 else np.float32(amax * np.float32(1 / 127))
+        step = np.float32(np.abs(x[r]).max() * np.float32(1 / 127))
+        s[r] = np.float32(1) if step == 0 else step
         q[r] = np.clip(np.rint(x[r] / s[r]), -127, 127).astype(np.int8)
     return q, s
 

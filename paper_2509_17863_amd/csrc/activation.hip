@@ -200,7 +200,9 @@ __global__ __launch_bounds__(kThreads) void quantize_int8_kernel(const uint16_t*
     }
     const bool finite = m < 0x7f800000u;
     const float amax = __uint_as_float(m);
-    const float sc = m == 0 ? 1.0f : finite ? amax * (1.0f / 127.0f) : __uint_as_float(0x7fc00000u);
+    // (the product is zero for a row of zeros, and below 2^-143 too)
+    const float step = amax * (1.0f / 127.0f);
+    const float sc = !finite ? __uint_as_float(0x7fc00000u) : step == 0.0f ? 1.0f : step;
     const float inv = __builtin_amdgcn_rcpf(sc);
     auto emit = [&](int ch, const float (&v)[8]) {
       // A product with the reciprocal is within 1e-4 of the quotient (at most 128, a

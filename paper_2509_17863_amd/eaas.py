@@ -570,7 +570,8 @@ def eaas_grouped_matmul_dw(dy: torch.Tensor, x: torch.Tensor, offsets: torch.Ten
 
 def eaas_quantize_rows_int8(x: torch.Tensor, q: torch.Tensor, s: torch.Tensor,
                             stream=None) -> None:
-    """x [rows, K] bf16 -> q [rows, K] int8 and s [rows] fp32 (s = amax * fp32(1/127)).
+    """x [rows, K] bf16 -> q [rows, K] int8 and s [rows] fp32 (s = amax * fp32(1/127),
+    1 where that is zero).
     Weights [E, N, K] are quantized per output channel as E*N rows."""
     rows, K = x.shape
     xp, ldx = _rows(x, K, torch.bfloat16)

@@ -43,6 +43,21 @@ def test_gates_far_below_zero(gpu, gates, up, rows, I):
     assert (off <= 2.0 ** -16).all(), off.max()  # (2^-16: the quotient's own rounding)
 
 
+@pytest.mark.parametrize("rows,I", [(4, 24), (2050, 24), (3, 2056), (2, 20000)])
+def test_a_scale_below_the_smallest_number_counts_as_zero(gpu, rows, I):
+    """33 * 2^-149 at the most, a 127th of which rounds to zero."""
+    gu = torch.zeros((rows, 2 * I))
+    gu[:, :I] = -0.001
+    gu[:, I::2] = 2.0 ** -133
+    gu = gu.to(torch.bfloat16)
+    h = L.swiglu(gu.double().numpy())
+    assert 0 < np.abs(h).max() < 63 * TINY
+    q, s = swiglu_int8(gu)
+    assert (s == 1).all() and (q == 0).all()
+    qr, sr = L.quantize_rows_int8(h[:2])
+    assert (sr == 1).all() and (qr == 0).all()
+
+
 def test_other_extremes(gpu):
     """Gates of any size next to a gate of 1."""
     g = torch.tensor([[-3e38, -1000.0, -104.0, -86.0, 0.0, 1.0, 87.0, 1000.0]] * 3)
