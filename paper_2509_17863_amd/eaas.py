@@ -499,7 +499,8 @@ def _gather(x: torch.Tensor, R: int, perm, k: int) -> tuple[int | None, int]:
         return None, 1
     if x.shape[0] * k != R:
         raise ValueError(f"x has {x.shape[0]} tokens of {k} slots, expected {R} rows in all")
-    return _dense(perm, torch.int32, R), int(k)
+    # (a routing's arrays have one element at least)
+    return _dense(perm, torch.int32, R or perm.numel()), int(k)
 
 
 def eaas_grouped_workspace_bytes(R, E, N, K) -> int:
