@@ -182,8 +182,12 @@ def _p(t):
 
 def _stream(stream):
     if stream is None:
-        # (the handle alone: a torch Stream object costs 2.6 us more, a third of a small call)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        # (the handle alone: a torch Stream object costs 2.6 us more, a third of a small call;
+        # it is no public function, so another torch may not have it)
+        handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if handle is None:
+            return torch.cuda.current_stream().cuda_stream
+        return handle(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -32,3 +32,17 @@ def test_an_empty_batch_with_its_routing(E):
     with pytest.raises(ValueError):  # (the type still counts)
         eaas.eaas_grouped_matmul(z(0, H), off, z(E, 2 * I, H), z(0, 2 * I), ws,
                                  perm=r["perm"].long(), k=k, stream=0)
+
+
+def test_the_current_stream_without_the_handle_function(monkeypatch):
+    class Stream:
+        cuda_stream = 42
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 40 + device,
+                        raising=False)
+    assert eaas._stream(None) == 43
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: Stream)
+    assert eaas._stream(None) == 42
+    assert eaas._stream(7) == 7 and eaas._stream(Stream) == 42
