@@ -14,7 +14,7 @@ namespace eaas {
 // of its own; completion is counted with vmcnt.
 __device__ __forceinline__ void load_lds16(const i32x4& rsrc, uint32_t voff, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
-               :: "v"(voff), "s"(rsrc), "s"(lds) : "memory", "m0");
+               :: "v"(voff), "s"(rsrc), "s"(lds) : "memory");
 }
 
 // Raw buffer descriptor of `bytes` bytes from `base` (both wave-uniform).

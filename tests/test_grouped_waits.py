@@ -78,15 +78,3 @@ def test_no_lds_access_is_under_way_at_a_barrier(kernels):
     for name, lines in large.items():
         assert lines.count("s_barrier") >= 4, name
         assert under_way_at_barriers(lines) == [], name
-
-
-def test_inline_assembly_that_writes_m0_says_so():
-    """(The compiler keeps values of its own in m0 where it needs it.)"""
-    found = 0
-    for name in ("grouped.h", "grouped_fast.h", "grouped.hip", "grouped_fast.hip",
-                 "grouped_few.hip"):
-        for asm in re.findall(r"asm[^;]*?\);", (_build.CSRC / name).read_text(), re.S):
-            if re.search(r"s_mov_b32 m0\b", asm):
-                found += 1
-                assert re.search(r':[^:]*"m0"[^:]*\);$', asm), asm
-    assert found == 1
