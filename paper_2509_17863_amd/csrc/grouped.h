@@ -10,6 +10,8 @@
 // the sum's index): A across in kGradWeights, B across in both gradients.
 #pragma once
 
+#include <algorithm>
+
 #include "common.h"
 #include "gemm_common.h"
 #include "internal.h"
@@ -89,15 +91,25 @@ __device__ __forceinline__ void tile_of(int local, int mt, int nt, int& tm, int&
   tm = run * kGroupedRun + in - tn * here;
 }
 
+// The grid of a launch over `tiles` tiles, each in `splits` parts.  (A dimension of a
+// grid holds less than 2^32 threads, so many tiles lie along z too.)
+constexpr long long kGridX = 1 << 22;
+inline dim3 tile_grid(long long tiles, int splits) {
+  return dim3((unsigned)std::min(tiles, kGridX), (unsigned)splits,
+              (unsigned)((tiles + kGridX - 1) / kGridX));
+}
+
 // The tile of this workgroup; false if there is none.  kForward and kGradRows:
 // the groups' row tiles are counted from the offsets (on the device), NT threads
 // take consecutive groups each, and the thread whose groups hold the tile
 // publishes it.  `lds` holds NT / 64 + 4 ints.  (Ends with a barrier.)
 template <int DIR, int BI, int BJ, int NT>
 __device__ __forceinline__ bool find_tile(const GroupedParams& p, int* lds, GroupedTile& t) {
+  const int tile = blockIdx.x + blockIdx.z * (int)kGridX;
   if constexpr (DIR == kGradWeights) {
     const int mt = ceil_div(p.N, BI), nt = ceil_div(p.K, BJ);
-    const int id = xcd_window_remap(blockIdx.x, gridDim.x);
+    if (tile >= p.E * mt * nt) return false;
+    const int id = xcd_window_remap(tile, p.E * mt * nt);
     t.e = id / (mt * nt);
     int tm, tn;
     tile_of(id - t.e * mt * nt, mt, nt, tm, tn);
@@ -140,8 +152,8 @@ __device__ __forceinline__ bool find_tile(const GroupedParams& p, int* lds, Grou
     }
     const int nt = ceil_div(columns<DIR>(p), BJ);
     total *= nt;
-    if ((int)blockIdx.x < total) {
-      const int id = xcd_window_remap(blockIdx.x, total);
+    if (tile < total) {
+      const int id = xcd_window_remap(tile, total);
 #pragma unroll
       for (int q = 0; q < PER; ++q) {
         if (id >= before * nt && id < (before + count[q]) * nt) {

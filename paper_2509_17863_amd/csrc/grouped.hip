@@ -428,8 +428,8 @@ hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t str
   } else if (g.kernel == kFew) {
     if constexpr (DIR != kGradWeights) e = launch_grouped_few<DIR, I8>(p, g.bi, tiles, stream);
   } else {
-    hipLaunchKernelGGL((grouped_any_kernel<DIR, I8>), dim3((unsigned)tiles, (unsigned)p.splits),
-                       dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((grouped_any_kernel<DIR, I8>), tile_grid(tiles, p.splits), dim3(kThreads),
+                       0, stream, p);
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.splits == 1) return e;

@@ -210,8 +210,8 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
 
 template <int DIR, bool I8, int MB, int STAGES>
 hipError_t launch(const GroupedParams& p, long long tiles, hipStream_t stream) {
-  hipLaunchKernelGGL((grouped_few_kernel<DIR, I8, MB, STAGES>),
-                     dim3((unsigned)tiles, (unsigned)p.splits), dim3(kThreads), 0, stream, p);
+  hipLaunchKernelGGL((grouped_few_kernel<DIR, I8, MB, STAGES>), tile_grid(tiles, p.splits),
+                     dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
