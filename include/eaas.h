@@ -440,10 +440,11 @@ size_t eaas_grouped_workspace_bytes(const eaas_group_shape *s);
 
 /* y[r,:] = W[e] x[src(r),:] for the rows r of every group e.
  *   x [R or R/k, K] bf16 (ldx), w [E,N,K] bf16, y [R,N] bf16 or fp32 (ldy)
- * y must not overlap x or w.  Errors: INVALID_ARG (null pointer, size below its
- * least, ld below the width, k < 1 or R % k with perm, overlap, alignment),
- * UNSUPPORTED (E > 1024, N*K or, with perm, (R/k)*ldx above 2^31 - 1, an ld
- * above 2^22), WORKSPACE, HIP.  R = 0: nothing is enqueued. */
+ * y must not overlap x or w (rows side by side in one wider array do not).
+ * Errors: INVALID_ARG (null pointer, size below its least, ld below the width, k < 1
+ * or R % k with perm, overlap, alignment), UNSUPPORTED (E > 1024, N*K or, with perm,
+ * (R/k)*ldx above 2^31 - 1, an ld above 2^22), WORKSPACE, HIP.  R = 0: nothing is
+ * enqueued. */
 int eaas_grouped_matmul(const eaas_group_shape *s, const void *x, int64_t ldx,
                         const int32_t *perm, int32_t k, const int32_t *offsets,
                         const void *w, void *y, int64_t ldy, int y_dtype,

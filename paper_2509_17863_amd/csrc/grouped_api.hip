@@ -19,15 +19,22 @@ int hip_status(hipError_t e) { return e == hipSuccess ? EAAS_OK : EAAS_ERR_HIP; 
 
 bool aligned(const void* p, size_t n) { return (uintptr_t)p % n == 0; }
 
+// Rows of `width` bytes, `pitch` bytes apart.
 struct Span {
   uintptr_t at;
-  unsigned long long bytes;
+  unsigned long long bytes, pitch, width;
 };
 Span rows_span(const void* p, long long rows, long long ld, long long width, int esz) {
-  return {(uintptr_t)p, rows > 0 ? (unsigned long long)((rows - 1) * ld + width) * esz : 0};
+  return {(uintptr_t)p, rows > 0 ? (unsigned long long)((rows - 1) * ld + width) * esz : 0,
+          (unsigned long long)ld * esz, (unsigned long long)width * esz};
 }
 bool overlap(const Span& a, const Span& b) {
-  return a.at < b.at + b.bytes && b.at < a.at + a.bytes;
+  if (a.at >= b.at + b.bytes || b.at >= a.at + a.bytes) return false;
+  if (a.pitch != b.pitch) return true;
+  // rows of one wider array: side by side, or one over the other
+  const Span &lo = a.at <= b.at ? a : b, &hi = a.at <= b.at ? b : a;
+  const unsigned long long d = (hi.at - lo.at) % lo.pitch;
+  return d < lo.width || d + hi.width > lo.pitch;
 }
 
 int check_group(const eaas_group_shape* s) {
