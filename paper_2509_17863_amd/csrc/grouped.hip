@@ -454,6 +454,11 @@ size_t grouped_workspace_most(const GroupedArgs& a) {
   return std::max(plan_bytes(a, grouped_plan(a, true)), plan_bytes(a, grouped_plan(a, false)));
 }
 
+int grouped_plan_code(const GroupedArgs& a, bool in16) {
+  const GroupedPlan g = grouped_plan(a, in16);
+  return g.kernel + 4 * g.bi + 4096 * g.splits;
+}
+
 hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream) {
   GroupedParams p{};
   p.a = static_cast<const char*>(a.a);

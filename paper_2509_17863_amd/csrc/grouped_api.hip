@@ -299,4 +299,14 @@ int eaas_unpermute_combine_backward(const eaas_shape* s, const void* dout, int d
                                             reinterpret_cast<hipStream_t>(stream)));
 }
 
+// Not part of the ABI: the kernel that a product takes, for tests and measurements
+// (grouped_plan_code), or -1 for what the library rejects.  dir: 0 forward, 1 gradient
+// in the rows, 2 in the weights; i8: in 8-bit integers; in16: sizes, strides and bases
+// in multiples of 16 bytes.
+int eaas_internal_grouped_plan(const eaas_group_shape* s, int dir, int i8, int in16) {
+  if (check_group(s) != EAAS_OK || dir < kForward || dir > kGradWeights || (i8 && dir != kForward))
+    return -1;
+  return grouped_plan_code(args_of(s, dir, i8 != 0), in16 != 0);
+}
+
 }  // extern "C"

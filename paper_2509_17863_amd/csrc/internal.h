@@ -169,6 +169,9 @@ size_t grouped_workspace(const GroupedArgs& a);
 // At most, for any strides and alignment (a's sizes only).
 size_t grouped_workspace_most(const GroupedArgs& a);
 hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream);
+// The kernel chosen (0 any alignment, 1 few rows, 2 large tiles) + 4 * rows of its
+// tiles + 4096 * parts of the sum; in16: everything in multiples of 16 bytes.
+int grouped_plan_code(const GroupedArgs& a, bool in16);
 
 // Activation, 8-bit rows and the combine's gradient (activation.hip).
 hipError_t launch_swiglu(const uint16_t* gu, long long rows, int I, const int32_t* n_rows,

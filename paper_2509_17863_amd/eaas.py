@@ -128,6 +128,8 @@ def _bind(L: ctypes.CDLL) -> ctypes.CDLL:
                                          i32, vp, sz, vp]
     L.eaas_grouped_matmul_int8.argtypes = [gp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, i64,
                                            i32, vp, sz, vp]
+    L.eaas_internal_grouped_plan.argtypes = [gp, i32, i32, i32]
+    L.eaas_internal_grouped_plan.restype = i32
     L.eaas_quantize_rows_int8.argtypes = [vp, i64, i64, ctypes.c_int32, vp, vp, vp]
     L.eaas_swiglu.argtypes = [vp, i64, ctypes.c_int32, vp, vp, vp]
     L.eaas_swiglu_int8.argtypes = [vp, i64, ctypes.c_int32, vp, vp, vp, vp]
@@ -505,6 +507,22 @@ def _gather(x: torch.Tensor, R: int, perm, k: int) -> tuple[int | None, int]:
         raise ValueError(f"x has {x.shape[0]} tokens of {k} slots, expected {R} rows in all")
     # (a routing's arrays have one element at least)
     return _dense(perm, torch.int32, R or perm.numel()), int(k)
+
+
+_GROUPED_KERNELS = ("any", "few", "large")
+
+
+def _grouped_plan(product: str, R, E, N, K, in16: bool) -> tuple[str, int, int]:
+    """(kernel, rows of its tiles, parts of the sum) of the product "forward", "dx",
+    "dw" or "int8": the library's own choice, asked on the host, for tests and
+    measurements.  in16: sizes, strides and bases are multiples of 16 bytes."""
+    s = _group_shape(R, E, N, K)
+    d = ("forward", "dx", "dw").index("forward" if product == "int8" else product)
+    r = int(lib().eaas_internal_grouped_plan(ctypes.byref(s), d, int(product == "int8"),
+                                             int(in16)))
+    if r < 0:
+        raise EaasError(-2, "eaas_internal_grouped_plan")
+    return _GROUPED_KERNELS[r & 3], (r & 4095) >> 2, r >> 12
 
 
 def eaas_grouped_workspace_bytes(R, E, N, K) -> int:

@@ -120,9 +120,10 @@ SHAPES = [
 ]
 
 
-# groups of many rows and matrices large enough for the 256 x 256 tiles (forward,
-# gradient in the rows: N resp. K wide; gradient in the weights: both), rows and
-# columns that end inside one, sums that end inside a step, more tiles than CUs
+# groups of many rows, rows and columns that end inside a 256 x 256 tile, sums that end
+# inside a step: the gradient in the weights takes those tiles here, the gradient in
+# the rows in one case, other products the other kernels (test_gpu_grouped_plans.py has
+# shapes for each kernel by name, and results of more tiles than CUs)
 LARGE = [
     (1500, 3, 6200, 72, "ragged", 0, 0),
     (1040, 2, 9000, 136, "even", 4, 8),
@@ -132,8 +133,9 @@ LARGE = [
 ]
 
 
-# the large tiles again where the sum is of some steps, in every direction (8-bit
-# included) and with empty groups; and sums of one to many parts
+# sums of some steps, which take the large tiles in every direction (8-bit included),
+# with empty groups; and sums of one to many parts (whose tolerance grows with the
+# length of the sum; test_gpu_grouped_plans.py has exact ones)
 LONGER = [
     (1200, 4, 8200, 464, "some", 0, 0),
     (1040, 2, 9000, 528, "even", 4, 8),
