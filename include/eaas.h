@@ -505,7 +505,8 @@ int eaas_swiglu(const void *gu, int64_t rows, int32_t I, const int32_t *n_rows, 
                 void *stream);
 
 /* The same, quantized as by eaas_quantize_rows_int8 instead of rounded to bf16
- * (codes and scales are those of the fp32 h): q [rows,I] int8, s [rows] fp32. */
+ * (codes and scales are those of the fp32 h, which is within about two units in its
+ * last place, for gates of any size): q [rows,I] int8, s [rows] fp32. */
 int eaas_swiglu_int8(const void *gu, int64_t rows, int32_t I, const int32_t *n_rows, void *q,
                      float *s, void *stream);
 

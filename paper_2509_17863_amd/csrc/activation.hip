@@ -3,10 +3,10 @@
 // the gradient of the weighted combine.  All of it is bound by memory: each value
 // is read once and written once, 16 bytes a lane, and what a row needs as a whole
 // (its largest magnitude, its inner product) is reduced while the row stays in
-// registers.  32768 rows of 2048: h in 70 us (5.7 TB/s), its gradient 118 (5.7), as
-// 8-bit rows 101 (3.3: the exponential and quotient of full precision bound it),
-// bf16 rows to 8 bits 43 (4.7); the combine's gradient, 4096 tokens of 8 slots, 7168
-// wide: 296 (5.0).
+// registers.  32768 rows of 2048: h in 73 us (5.5 TB/s), its gradient 118 (5.7), as
+// 8-bit rows 77 (4.4: 41 vector instructions a value, which take 82% of the cycles), bf16
+// rows to 8 bits 39 (5.1); the combine's gradient, 4096 tokens of 8 slots, 7168 wide:
+// 296 (5.0).
 #include <algorithm>
 
 #include "common.h"
@@ -261,7 +261,7 @@ hipError_t launch_int8(const uint16_t* x, long long ldx, long long rows, int K,
   };
   // A wave to a row where there are rows enough to fill the chip with them (no
   // barrier, and a lane's chunks are loaded together): 65536 rows of 768 in 59 us
-  // against 98 with a workgroup to a row, 32768 of 2048 in 101 against 110; else a
+  // against 102 with a workgroup to a row, 32768 of 2048 in 77 against 82; else a
   // workgroup to a row.
   if (rows >= 2048 && K <= 2048) {
     if (K <= 512) return go(quantize_int8_kernel<SWIGLU, 64, 1>, 64);

@@ -16,8 +16,8 @@
 //
 // What bounds it: loads that straddle lines (a wave's 16-byte loads take 7.6 ns on
 // aligned rows, 13.8 where rows start on any dword, 27 on any 2 bytes), then LDS.
-// 8 experts of 1024 rows, 4097 x 8191: forward 0.85 ms (648 TFLOP/s), dx 0.92, dW
-// 0.95; 8-bit integers 0.54 (1019 TOP/s).
+// 8 experts of 1024 rows, 4097 x 8191: forward 0.90 ms (608 TFLOP/s), dx 0.96, dW
+// 0.94; 8-bit integers 0.54 (1025 TOP/s).
 #include <algorithm>
 
 #include "grouped_fast.h"
@@ -366,21 +366,27 @@ int best_parts(int steps, double out, F&& us, double* time) {
 }
 
 // The choice.  Two regions are taken before the estimates, which know no memory
-// traffic; both sides measured (us, rows of each group x E groups, N x K):
+// traffic; both sides measured (us, rows of each group x E groups, N x K, bf16 results):
 //   Large tiles on every CU, groups of some rows and a sum of some steps: they read
 //   the weights as fast as the few-rows kernel, and each byte once.  dx 24 x 32, 4096
-//   x 7168: 362 large, 370 few; 16 x 128, 1536 x 2048: 151, 175; 8-bit 24 x 32: 172,
-//   187; forward 64 x 32: 346, 373, but 32 x 128: 195, 182.  2500 x 16, 4096 x 512
-//   (8 steps): 123 large, 174 any; but 482 x 19, 2208 x 160 (3 steps): 33, 23.
-//   dW 128 x 32, 2048 x 2048: 100 large, 131 any; 64 x 128, 1536 x 2048: 274, 270;
-//   on fewer large tiles than CUs 4096 x 1, 1024 x 4096 (64 tiles): 78 large, 180 any;
-//   4096 x 8, 256 x 256 (8 tiles): 74, 29.
+//   x 7168: 349 large, 367 few; 16 x 128, 1536 x 2048: 148, 175; 8-bit 24 x 32: 165,
+//   183; forward 64 x 32: 318, 369, but 32 x 128: 190, 177.  2500 x 16, 4096 x 512
+//   (8 steps): 172 large, 238 any; but 482 x 19, 2208 x 160 (3 steps): 32, 22.
+//   dW 128 x 32, 2048 x 2048: 68 large, 83 any; 64 x 128, 1536 x 2048: 147 large, 172
+//   any (fp32: 274, 257); on fewer large tiles than CUs 4096 x 1, 1024 x 4096 (64 tiles):
+//   75 large, 79 any in one part (61 in two: the rule looks at neither sums that long
+//   nor parts; 131072 x 1, 1792 x 1792: 2172, in two parts 1598); 4096 x 8, 256 x 256 (8
+//   tiles): 72 large, 22 any in 8 parts.
 //   Groups of one to 24 rows, a sum of some steps: tiles of 16 or 32 rows, which the
-//   others would leave mostly empty.  20 x 8, 4096 x 4096, forward: 45 few, 52 any in 3 parts,
-//   63 large; 14 x 53, 160 x 3600, dx (3 steps): 50 few, 24 any.
-// What the estimates decide: forward 200 x 1, 1024 x 1024: 9 few in one part, 12 in
-// 4; 215 x 3, 464 x 12176: 35 any in 16 parts, 45 few in 4; 2500 x 4, 512 x 8192:
-// 128 large, 137 any in 2 parts, 139 few.
+//   others would leave mostly empty.  20 x 8, 4096 x 4096, forward: 43 few, 53 any in 3 parts,
+//   63 large; 14 x 53, 160 x 3600, dx (3 steps): 49 few, 23 any.
+// What the estimates decide: forward 200 x 1, 1024 x 1024: 8 few in one part, 11 in
+// 4; 215 x 3, 464 x 12176: 38 few in 2 parts, 34 any in 16, 45 few in 4; 2500 x 4, 512 x
+// 8192: 127 large, 130 any in 2 parts, 132 few.
+// A group's rows are the mean over the groups that could have any: rows that fall on
+// few of many groups take tiles for the mean.  Forward, 256 rows on 1 of 32, 4096 x
+// 7168: 56 on tiles of 16 rows, 31 on 64; 96 rows on each of 16 of 128, 2048 x 2048: 63,
+// large 39; but 64 on each of 8 of 128, 1536 x 2048: 20, 21 on 64, 29 large.
 GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   const long long rows = a.R / std::max(1, std::min(a.R, a.E));  // of a group that has any
   const long long sum = a.dir == kForward ? a.K : a.dir == kGradRows ? a.N : rows;

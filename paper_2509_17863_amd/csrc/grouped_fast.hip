@@ -26,9 +26,9 @@
 // rows of the sum in dW.)  Row tiles come from a table that a small kernel makes
 // from the groups' offsets.
 //
-// What bounds it: long sums the power limit (8192^3: 0.80 ms forward, 0.82 dx, 0.80
+// What bounds it: long sums the power limit (8192^3: 0.80 ms forward, 0.81 dx, 0.83
 // dW, 1.37 PFLOP/s, at 1.44 GHz with the matrix pipes busy 83% of cycles; 8-bit
-// integers 0.43 ms, 2.5 POP/s); short ones the 7 us a tile that are left of start,
+// integers 0.44 ms, 2.5 POP/s); short ones the 7 us a tile that are left of start,
 // way out and stores (8 experts of 1024 rows, 4096 x 14336, dW fp32: 0.94 ms, 1.02
 // PFLOP/s; 1.5 us for each 64 rows of the sum).
 //
