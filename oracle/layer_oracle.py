@@ -120,3 +120,69 @@ def combine_backward(dout, y, inv, weights):
                 dw[t, j] = (dout[t] * y[r]).sum()
                 mag[t, j] = np.abs(dout[t] * y[r]).sum()
     return dy, dw, mag
+
+
+def e4m3_values():
+    """The value of each of the 256 codes (NaN for the two that stand for none)."""
+    code = np.arange(256)
+    m, e = code & 7, (code >> 3) & 15
+    v = np.where(e > 0, (8 + m) * 2.0 ** (e - 10.0), m * 2.0 ** -9)
+    v = np.where((code & 127) == 127, np.nan, v)
+    return np.where(code >= 128, -v, v)
+
+
+def e4m3_codes(x):
+    """Codes nearest to x, ties to the even code, saturated at +-448."""
+    v = e4m3_values()[:127]                        # 0 .. 448, ascending
+    a = np.minimum(np.abs(np.asarray(x, np.float64)), 448.0)
+    hi = np.clip(np.searchsorted(v, a), 0, 126)    # v[hi - 1] < a <= v[hi]
+    lo = np.maximum(hi - 1, 0)
+    up = v[hi] - a < a - v[lo]
+    tie = v[hi] - a == a - v[lo]
+    c = np.where(up | (tie & (hi % 2 == 0)), hi, lo)
+    return (c | (np.signbit(x).astype(int) << 7)).astype(np.uint8)
+
+
+def quantize_blocks(x, block_rows=1):
+    """(codes, scales) of an fp32 matrix: a scale for each block of block_rows x 128,
+    amax / 448 in fp32 (1 where that is zero), quotients in fp32; NaN and zero codes for a
+    block that holds an infinity or a NaN."""
+    x = np.asarray(x, np.float32)
+    n, K = x.shape
+    nb, kb = -(-n // block_rows), -(-K // 128)
+    q, s = np.zeros((n, K), np.uint8), np.zeros((nb, kb), np.float32)
+    for i in range(nb):
+        for j in range(kb):
+            at = np.s_[i * block_rows: (i + 1) * block_rows, j * 128: (j + 1) * 128]
+            b = x[at]
+            if not np.isfinite(b).all():
+                s[i, j] = np.nan
+                continue
+            sc = np.float32(np.abs(b).max() / np.float32(448))
+            s[i, j] = np.float32(1) if sc == 0 else sc
+            q[at] = e4m3_codes(b / s[i, j])
+    return q, s
+
+
+def dequantized(q, s, block_rows=1):
+    full = np.repeat(np.repeat(s.astype(np.float64), block_rows, 0), 128, 1)
+    return e4m3_values()[q] * full[: q.shape[0], : q.shape[1]]
+
+
+def grouped_matmul_fp8(xq, xs, offsets, wq, wscale, src):
+    """(y, sum of the magnitudes of its terms)."""
+    w = np.stack([dequantized(wq[e], wscale[e], 128) for e in range(len(wq))])
+    return grouped_matmul(dequantized(xq, xs), offsets, w, src)
+
+
+def grouped_swiglu(x, offsets, w, src):
+    """(h, gate and up sums, the sums of their terms' magnitudes) for w [E, 2I, K]."""
+    gu, mag = grouped_matmul(x, offsets, w, src)
+    return swiglu(gu), gu, mag
+
+
+def grouped_swiglu_backward(dy, offsets, w, gu):
+    """(dgu, h, dh, the sum of the magnitudes of dh's terms) for w [E, N, I]."""
+    dh, mag = grouped_matmul_dx(dy, offsets, w)
+    gu = gu[: len(dh)]
+    return swiglu_backward(gu, dh), swiglu(gu), dh, mag

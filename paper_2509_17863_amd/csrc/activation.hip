@@ -9,86 +9,13 @@
 // 296 (5.0).
 #include <algorithm>
 
-#include "common.h"
 #include "internal.h"
+#include "swiglu.h"
 
 namespace eaas {
 namespace {
 
 constexpr int kThreads = 256;
-
-// Eight bf16 at an address of 2-byte alignment, n of them valid (zeros after).
-__device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    u32x4 raw;
-    __builtin_memcpy(&raw, p, 16);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(raw[i] << 16);
-      v[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? __uint_as_float((uint32_t)p[i] << 16) : 0.0f;
-  }
-}
-
-__device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) {
-  if (n >= 8) {
-    u32x4 o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)  // (one instruction a pair)
-      o[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)v[2 * i], (__bf16)v[2 * i + 1]});
-    __builtin_memcpy(p, &o, 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (uint16_t)f32_to_bf16_bits(v[i]);
-  }
-}
-
-// 1 / (1 + exp(-g)) as a product hi * lo: with z = exp(-|g| / 2) it is z * (z / (1 +
-// z^2)) for g < 0 and 1 * (1 / (1 + z^2)) otherwise, so a gate far below zero,
-// whose sigmoid alone is under the normal range of fp32, keeps its precision
-// until the product with the gate is taken.  The hardware exponential and
-// reciprocal err by a few units in the last place of fp32, far below the rounding
-// of the results to bf16.
-struct Sigmoid {
-  float hi, lo;
-};
-__device__ __forceinline__ Sigmoid sigmoid(float g) {
-  const float z = __expf(-0.5f * fabsf(g));
-  const float r = __builtin_amdgcn_rcpf(1.0f + z * z);
-  return g < 0.0f ? Sigmoid{z, z * r} : Sigmoid{1.0f, r};
-}
-
-__device__ __forceinline__ float silu_up(float g, float up) {
-  const Sigmoid t = sigmoid(g);
-  return (g * t.hi) * t.lo * up;
-}
-
-// g / (1 + exp(-g)) from a gate of kFar or more, to about two units in the last place:
-// the full exponential and its sum with 1 are rounded, the quotient is corrected by
-// its remainder.  (The reciprocal is a normal number there.)
-constexpr float kFar = -86.0f;
-__device__ __forceinline__ float silu_full(float g) {
-  const float d = 1.0f + expf(-g);
-  const float y = __builtin_amdgcn_rcpf(d);
-  const float q = g * y;
-  return fmaf(fmaf(-q, d, g), y, q);
-}
-
-// The same times up, below kFar: the quotient is g exp(g) to fp32, whose exponential
-// leaves the normal range from -87.3 on; two factors exp(g / 2) do not, and each takes
-// its share of the product.
-__device__ __forceinline__ float silu_far_up(float g, float up) {
-  const float z = expf(0.5f * g);
-  return (g * z) * (z * up);
-}
-
-__device__ __forceinline__ long long live_rows(long long rows, const int32_t* n_rows) {
-  return n_rows ? min(rows, (long long)max(*n_rows, 0)) : rows;
-}
 
 // One thread: eight columns of a row.
 template <bool BACKWARD>
@@ -115,9 +42,9 @@ __global__ __launch_bounds__(kThreads) void swiglu_kernel(const uint16_t* gu, co
       load8(dh + r * I + c, n, d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const Sigmoid t = sigmoid(g[i]);
-        o[i] = d[i] * up[i] * t.hi * (t.lo * (1.0f + g[i] * (1.0f - t.hi * t.lo)));
-        o2[i] = (d[i] * g[i] * t.hi) * t.lo;
+        const SwigluGrad t = swiglu_grad(g[i], up[i], d[i]);
+        o[i] = t.gate;
+        o2[i] = t.up;
       }
       store8(out + r * 2 * I + c, n, o);
       store8(out + r * 2 * I + I + c, n, o2);

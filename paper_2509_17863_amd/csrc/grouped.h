@@ -8,6 +8,18 @@
 // Operand A holds the i side and operand B the j side.  An operand lies either
 // along the sum (its memory rows are i or j) or across it (its memory rows are
 // the sum's index): A across in kGradWeights, B across in both gradients.
+//
+// Two products have an epilogue that is not the identity:
+//   kSwiglu (kForward)       W is [W_gate; W_up] by rows, N = 2I.  A column tile holds as
+//                            many gate rows of W as up rows, those of the same columns
+//                            of h, so that the two sums a value of h needs meet in one
+//                            lane.  Columns of the result are those of h, 0 .. I-1.
+//   kSwigluGrad (kGradRows)  the sums are dh, which is not stored: gate and up are read
+//                            and their gradients written (and h, for the gradient of
+//                            the matrix that h went into).
+// Operands of 8 bits are kInt8 (sums in int32, scaled once at the end) or kFp8, whose
+// scales change every 128 elements of the sum: the sum over such a block is taken by
+// itself and then added, scaled, to the sum at hand.
 #pragma once
 
 #include <algorithm>
@@ -15,6 +27,7 @@
 #include "common.h"
 #include "gemm_common.h"
 #include "internal.h"
+#include "swiglu.h"
 
 namespace eaas {
 
@@ -39,16 +52,21 @@ struct GroupedParams {
   bool vec;               // out may be stored four columns at a time
   bool vec16;             // and 16 bytes at a time
   bool accumulate;        // kGradWeights: out += (fp32)
-  const float* row_scale; // 8-bit integers: of x's rows
-  const float* col_scale; // [E,N]
+  const float* row_scale; // kInt8: of x's rows; kFp8: [rows, ceil(K/128)]
+  const float* col_scale; // kInt8: [E,N]; kFp8: [E, ceil(N/128), ceil(K/128)]
+  uint16_t* gu;           // kSwiglu: gets the sums, or nullptr; kSwigluGrad: read
+  long long ldgu;
+  uint16_t* h;            // kSwigluGrad: written, or nullptr
+  long long ldh;
   int splits;             // the sum in this many parts, to `part` if more than one
   i32x4* row_tiles;       // large tiles: the row tiles of all groups (in the workspace)
   void* part;             // [splits][rows of out][columns] fp32 (8-bit: int32)
 };
 
-template <int DIR>
+// Columns of the result (kSwiglu: of h; kSwigluGrad: of dh).
+template <int DIR, int EPI = kPlain>
 __device__ __forceinline__ int columns(const GroupedParams& p) {
-  return DIR == kForward ? p.N : p.K;
+  return DIR != kForward ? p.K : EPI == kSwiglu ? p.N / 2 : p.N;
 }
 
 __device__ __forceinline__ void group_range(const GroupedParams& p, int e, int& beg, int& end) {
@@ -103,7 +121,7 @@ inline dim3 tile_grid(long long tiles, int splits) {
 // the groups' row tiles are counted from the offsets (on the device), NT threads
 // take consecutive groups each, and the thread whose groups hold the tile
 // publishes it.  `lds` holds NT / 64 + 4 ints.  (Ends with a barrier.)
-template <int DIR, int BI, int BJ, int NT>
+template <int DIR, int BI, int BJ, int NT, int EPI = kPlain>
 __device__ __forceinline__ bool find_tile(const GroupedParams& p, int* lds, GroupedTile& t) {
   const int tile = blockIdx.x + blockIdx.z * (int)kGridX;
   if constexpr (DIR == kGradWeights) {
@@ -150,7 +168,7 @@ __device__ __forceinline__ bool find_tile(const GroupedParams& p, int* lds, Grou
       before += w < wave ? lds[w] : 0;
       total += lds[w];
     }
-    const int nt = ceil_div(columns<DIR>(p), BJ);
+    const int nt = ceil_div(columns<DIR, EPI>(p), BJ);
     total *= nt;
     if (tile < total) {
       const int id = xcd_window_remap(tile, total);
@@ -222,6 +240,42 @@ __device__ __forceinline__ f32x4 scaled(const GroupedParams& p, int e, float rs,
   for (int c = 0; c < 4; ++c)
     o[c] = (float)v[c] * rs * (j + c < p.N ? p.col_scale[(size_t)e * p.N + j + c] : 0.0f);
   return o;
+}
+
+// Columns j.. of row i of a product with an epilogue, eight or the n < 8 that exist, at
+// any alignment.  kSwiglu: h, and the sums where they are kept.
+__device__ __forceinline__ void store_swiglu(const GroupedParams& p, size_t i, int j, int n,
+                                             const float (&g)[8], const float (&u)[8]) {
+  float h[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) h[c] = silu_up(g[c], u[c]);
+  store8(static_cast<uint16_t*>(p.out) + i * p.ldo + j, n, h);
+  if (p.gu) {
+    uint16_t* at = p.gu + i * p.ldgu + j;
+    store8(at, n, g);
+    store8(at + p.N / 2, n, u);
+  }
+}
+
+// kSwigluGrad, from dh.  (The result may lie over gate and up: they are read before.)
+__device__ __forceinline__ void store_swiglu_grad(const GroupedParams& p, size_t i, int j, int n,
+                                                  const float (&dh)[8]) {
+  const uint16_t* from = p.gu + i * p.ldgu + j;
+  float g[8], u[8];
+  load8(from, n, g);
+  load8(from + p.K, n, u);
+  float dg[8], du[8], h[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const SwigluGrad t = swiglu_grad(g[c], u[c], dh[c]);
+    dg[c] = t.gate;
+    du[c] = t.up;
+    h[c] = silu_up(g[c], u[c]);
+  }
+  uint16_t* to = static_cast<uint16_t*>(p.out) + i * p.ldo + j;
+  store8(to, n, dg);
+  store8(to + p.K, n, du);
+  if (p.h) store8(p.h + i * p.ldh + j, n, h);
 }
 
 // grouped_fast.hip: 256 x 256 tiles, sizes and addresses in multiples of 16 bytes.

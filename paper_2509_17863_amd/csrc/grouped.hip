@@ -1,6 +1,6 @@
 // Grouped products of an expert's matrix, for any size, stride and alignment:
-// forward, gradient in the rows, gradient in the weights, and the forward in
-// 8-bit integers (grouped.h states the three products in one frame).
+// forward, gradient in the rows, gradient in the weights, the forward in 8-bit integers
+// and in e4m3, and the two with an epilogue (grouped.h states them in one frame).
 //
 // A workgroup of four waves computes a tile of 128 x 128 results; a wave holds
 // 64 x 64 of them as 2 x 2 blocks of v_mfma_f32_32x32x16_bf16 (8-bit integers:
@@ -142,21 +142,43 @@ __device__ __forceinline__ u32x4 fragment(const LDS_AS char* stage, int c0, int 
   }
 }
 
-template <int DIR, bool I8>
+// The sum over a block of 128 e4m3 elements for 32 rows from a0 and 32 columns from b0:
+// codes go to bf16, which holds them exactly, products of those are exact in fp32 and are
+// summed there.  (The 8-bit floating matrix instructions keep less: see grouped_fp8.hip.)
+// A lane's 16 codes make two steps of the sum, whose order both operands share.
+__device__ __forceinline__ f32x16 fp8_block(const LDS_AS char* sa, int a0, const LDS_AS char* sb,
+                                            int b0) {
+  f32x16 part = {};
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) {
+    const u32x4 a = fragment<false>(sa, a0, kk), b = fragment<false>(sb, b0, kk);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          fp8x8_to_bf16(u32x2{b[2 * h], b[2 * h + 1]}), fp8x8_to_bf16(u32x2{a[2 * h], a[2 * h + 1]}),
+          part, 0, 0, 0);
+  }
+  return part;
+}
+
+template <int DIR, int TYPE, int EPI>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3)))
 void grouped_any_kernel(GroupedParams p) {
   constexpr bool A_ACROSS = DIR == kGradWeights, B_ACROSS = DIR != kForward;
-  constexpr int ESZ = I8 ? 1 : 2;
-  constexpr int SUM = 128 / ESZ;  // the sum's elements in a tile
-  static_assert(!I8 || DIR == kForward, "8-bit integers: forward only");
+  constexpr bool I8 = TYPE == kInt8, FP8 = TYPE == kFp8;
+  constexpr int ESZ = TYPE == kBf16 ? 2 : 1;
+  constexpr int SUM = 128 / ESZ;  // the sum's elements in a tile (kFp8: a block of scales)
+  constexpr int kBJ = EPI == kSwiglu ? eaas::kBJ / 2 : eaas::kBJ;  // columns of a result tile
+  static_assert(TYPE == kBf16 || DIR == kForward, "8-bit operands: forward only");
+  static_assert(EPI == kPlain || TYPE == kBf16, "epilogues: bf16 operands only");
   constexpr int kWaves = kThreads / kWave;
   constexpr int kLds = std::max(2 * kStage, kWaves * kWayOutBytes);
   __shared__ __attribute__((aligned(16))) char smem[kLds];
   __shared__ int s_find[kThreads / kWave + 4];
   GroupedTile t;
-  if (!find_tile<DIR, kBI, kBJ, kThreads>(p, s_find, t)) return;
+  if (!find_tile<DIR, kBI, kBJ, kThreads, EPI>(p, s_find, t)) return;
 
-  const int cols = columns<DIR>(p);
+  const int cols = columns<DIR, EPI>(p);
   const int sum_end = DIR == kForward ? p.K : DIR == kGradRows ? p.N : t.end - t.beg;
   const int tiles = ceil_div(sum_end, SUM);
   const int split = blockIdx.y;
@@ -172,6 +194,10 @@ void grouped_any_kernel(GroupedParams p) {
   };
   int src[4];  // kGradWeights: this thread's rows of x in the next tile to load
   auto b_row = [&](int q, int j) {
+    if (EPI == kSwiglu) {  // 32 gate rows, the 32 up rows of the same columns, and again
+      const int col = min(t.j0 + (j >> 6) * 32 + (j & 31), cols - 1);
+      return w + (size_t)(col + (j & 32 ? cols : 0)) * p.ldb * ESZ;
+    }
     if (DIR == kForward) return w + (size_t)min(t.j0 + j, cols - 1) * p.ldb * ESZ;
     if (DIR == kGradRows) return w + (size_t)j * p.ldb * ESZ;
     return w + (size_t)src[q] * p.ldb * ESZ;
@@ -203,6 +229,18 @@ void grouped_any_kernel(GroupedParams p) {
   const int wi = (wave & 1) * 64, wj = (wave >> 1) * 64;
   LDS_AS char* lds = (LDS_AS char*)smem;
 
+  // kFp8: the scales of this wave's rows (one a lane and block of rows) and of the tile's
+  // columns, which lie in one block of 128
+  const int kb = FP8 ? ceil_div(p.K, 128) : 0;
+  const float *row_scale[2], *col_scale = nullptr;
+  if constexpr (FP8) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      row_scale[i] = p.row_scale + (size_t)source_row(p, t.i0 + min(wi + 32 * i + (int)(threadIdx.x & 31),
+                                                                   t.i_valid - 1)) * kb;
+    col_scale = p.col_scale + ((size_t)t.e * ceil_div(p.N, 128) + t.j0 / 128) * kb;
+  }
+
   if (first < last) {
     find_rows(first);
     load(first);
@@ -212,6 +250,23 @@ void grouped_any_kernel(GroupedParams p) {
       __syncthreads();
       if (kt + 1 < last) load(kt + 1);
       const LDS_AS char *sa = lds, *sb = lds + kStage;
+      if constexpr (FP8) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float f = row_scale[i][kt] * col_scale[kt];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const f32x16 part = fp8_block(sa, wi + 32 * i, sb, wj + 32 * j);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = fmaf(part[v], f, acc[i][j][v]);
+            // (one block at a time: with the fragments of all four read ahead, 300
+            // registers went to memory)
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        __syncthreads();
+        continue;
+      }
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk) {
         u32x4 fa[2], fb[2];
@@ -238,15 +293,19 @@ void grouped_any_kernel(GroupedParams p) {
   }
 
   // (the last barrier is behind every wave's fragment reads)
-  way_out<DIR, I8>(p, t, split, wi, t.j0 + wj, acc,
-                   (LDS_AS float*)(smem + wave * kWayOutBytes));
+  LDS_AS float* buf = (LDS_AS float*)(smem + wave * kWayOutBytes);
+  if constexpr (EPI == kPlain)
+    way_out<DIR, TYPE>(p, t, split, wi, t.j0 + wj, acc, buf);
+  else
+    way_out_swiglu<DIR, EPI>(p, t, split, wi, t.j0 + (EPI == kSwiglu ? wj / 2 : wj), acc, buf);
 }
 
 // The parts of a split sum joined, in ascending order: one thread for four
 // columns of one row (VEC: rows of whole quads, 16 bytes a part).  Parts are loaded
 // eight at a time.
-template <int DIR, bool I8, bool VEC>
+template <int DIR, int TYPE, bool VEC>
 __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p) {
+  constexpr bool I8 = TYPE == kInt8;
   typedef typename std::conditional<I8, i32x4, f32x4>::type Quad;
   typedef typename std::conditional<I8, int, float>::type One;
   const int cols = columns<DIR>(p);
@@ -293,12 +352,54 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p) {
   }
 }
 
+// The same for a product with an epilogue: one thread for eight columns of one row.
+template <int DIR, int EPI>
+__global__ __launch_bounds__(256) void grouped_join_swiglu_kernel(GroupedParams p) {
+  const int cols = columns<DIR, EPI>(p), wide = columns<DIR>(p);
+  const int units = ceil_div(cols, 8);
+  const long long first = min(max(p.offsets[0], 0), p.R);
+  const long long rows = min(max(p.offsets[p.E], 0), p.R);
+  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (rows - first) * units;
+       u += (long long)gridDim.x * 256) {
+    const long long row = first + u / units;
+    const int j = (int)(u % units) * 8, n = cols - j;
+    const float* part = static_cast<const float*>(p.part) + (size_t)row * wide + j;
+    float a[8] = {}, b[8] = {};
+    for (int s0 = 0; s0 < p.splits; s0 += 2) {
+      float x[2][8], y[2][8];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const float* at = part + (size_t)min(s0 + s, p.splits - 1) * p.R * wide;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          x[s][c] = at[min(c, n - 1)];
+          if constexpr (EPI == kSwiglu) y[s][c] = at[cols + min(c, n - 1)];
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        if (s0 + s < p.splits) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            a[c] += x[s][c];
+            if constexpr (EPI == kSwiglu) b[c] += y[s][c];
+          }
+        }
+    }
+    if constexpr (EPI == kSwiglu) store_swiglu(p, row, j, n, a, b);
+    else store_swiglu_grad(p, row, j, n, a);
+  }
+}
+
 // Row tiles of all groups together, at most: every group may end in a part tile.
 long long most_row_tiles(const GroupedArgs& a, int bi) {
   return a.R / bi + std::min(a.R, a.E);
 }
 
 long long out_tiles(const GroupedArgs& a, int bi, int bj) {
+  // (kSwiglu: a tile has as many columns of W's halves together as any other's)
+  if (a.dir == kForward && a.epilogue == kSwiglu)
+    return most_row_tiles(a, bi) * ceil_div(a.N / 2, bj / 2);
   if (a.dir == kForward) return most_row_tiles(a, bi) * ceil_div(a.N, bj);
   if (a.dir == kGradRows) return most_row_tiles(a, bi) * ceil_div(a.K, bj);
   return (long long)a.E * ceil_div(a.N, bi) * ceil_div(a.K, bj);
@@ -308,7 +409,7 @@ long long out_tiles(const GroupedArgs& a, int bi, int bj) {
 // multiples of 16 bytes (rows of W: K elements; the sum of kGradRows: N), and what
 // one descriptor covers below 2 GiB: 256 rows, or with perm all tokens.
 bool in_16_bytes(const GroupedArgs& a) {
-  const int m = a.i8 ? 16 : 8, esz = a.i8 ? 1 : 2;
+  const int m = a.type == kBf16 ? 8 : 16, esz = 16 / m;
   if (a.K % m || a.lda % m || (uintptr_t)a.a % 16 || (uintptr_t)a.b % 16) return false;
   const long long ldb = a.dir == kGradWeights ? a.ldb : a.K, most = 1LL << 31;
   if (256 * esz * std::max(a.lda, ldb) >= most) return false;
@@ -390,7 +491,7 @@ int best_parts(int steps, double out, F&& us, double* time) {
 GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   const long long rows = a.R / std::max(1, std::min(a.R, a.E));  // of a group that has any
   const long long sum = a.dir == kForward ? a.K : a.dir == kGradRows ? a.N : rows;
-  const int steps = ceil_div((int)sum, a.i8 ? 128 : 64);
+  const int steps = ceil_div((int)sum, a.type == kBf16 ? 64 : 128);
   const double out = a.dir == kGradWeights ? (double)a.E * a.N * a.K
                                            : (double)a.R * (a.dir == kForward ? a.N : a.K);
   const double tiles = (double)out_tiles(a, kBI, kBJ);
@@ -399,9 +500,9 @@ GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   GroupedPlan any{kAny, kBI, kBJ, 1};
   double t_any;
   any.splits = best_parts(steps, out, [&](int s) { return any_us(tiles, steps, s); }, &t_any);
-  if (!in16) return any;
+  if (!in16 || a.type == kFp8 || a.epilogue != kPlain) return any;
   if (a.dir == kGradWeights) return rows >= 128 && large >= 48 ? on_large : any;
-  const int some = a.dir == kForward && !a.i8 ? 48 : 16;
+  const int some = a.dir == kForward && a.type == kBf16 ? 48 : 16;
   if (rows >= some && large >= 192 && steps >= 4) return on_large;
   GroupedPlan few{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};
   const double cells = (double)out_tiles(a, few.bi, few.bj);
@@ -421,7 +522,7 @@ size_t plan_bytes(const GroupedArgs& a, const GroupedPlan& g) {
   return (size_t)g.splits * rows * (a.dir == kForward ? a.N : a.K) * 4;
 }
 
-template <int DIR, bool I8>
+template <int DIR, int TYPE, int EPI = kPlain>
 hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t stream) {
   const GroupedPlan g = grouped_plan(a, in_16_bytes(a));
   const long long tiles = out_tiles(a, g.bi, g.bj);
@@ -430,23 +531,29 @@ hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t str
   p.splits = g.splits;
   hipError_t e = hipSuccess;
   if (g.kernel == kLarge) {
-    e = launch_grouped_pp<DIR, I8>(p, tiles, stream);
+    if constexpr (EPI == kPlain && TYPE != kFp8)
+      e = launch_grouped_pp<DIR, TYPE == kInt8>(p, tiles, stream);
   } else if (g.kernel == kFew) {
-    if constexpr (DIR != kGradWeights) e = launch_grouped_few<DIR, I8>(p, g.bi, tiles, stream);
+    if constexpr (DIR != kGradWeights && EPI == kPlain && TYPE != kFp8)
+      e = launch_grouped_few<DIR, TYPE == kInt8>(p, g.bi, tiles, stream);
   } else {
-    hipLaunchKernelGGL((grouped_any_kernel<DIR, I8>), tile_grid(tiles, p.splits), dim3(kThreads),
-                       0, stream, p);
+    hipLaunchKernelGGL((grouped_any_kernel<DIR, TYPE, EPI>), tile_grid(tiles, p.splits),
+                       dim3(kThreads), 0, stream, p);
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.splits == 1) return e;
-  const int cols = DIR == kForward ? a.N : a.K;
+  const int cols = EPI == kSwiglu ? a.N / 2 : DIR == kForward ? a.N : a.K;
   const long long rows = DIR == kGradWeights ? (long long)a.E * a.N : a.R;
-  const long long blocks = (rows * ceil_div(cols, 4) + 255) / 256;
+  const long long blocks = (rows * ceil_div(cols, EPI == kPlain ? 4 : 8) + 255) / 256;
   const dim3 grid((unsigned)std::min<long long>(blocks, 4096)), block(256);
-  if (cols % 4 == 0)
-    hipLaunchKernelGGL((grouped_join_kernel<DIR, I8, true>), grid, block, 0, stream, p);
+  // (kFp8: the parts are scaled, and join as bf16 operands' do)
+  constexpr int JOIN = TYPE == kFp8 ? kBf16 : TYPE;
+  if constexpr (EPI != kPlain)
+    hipLaunchKernelGGL((grouped_join_swiglu_kernel<DIR, EPI>), grid, block, 0, stream, p);
+  else if (cols % 4 == 0)
+    hipLaunchKernelGGL((grouped_join_kernel<DIR, JOIN, true>), grid, block, 0, stream, p);
   else
-    hipLaunchKernelGGL((grouped_join_kernel<DIR, I8, false>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((grouped_join_kernel<DIR, JOIN, false>), grid, block, 0, stream, p);
   return hipGetLastError();
 }
 
@@ -490,12 +597,19 @@ hipError_t launch_grouped(const GroupedArgs& a, hipStream_t stream) {
   p.k_shift = shift - 1;
   p.row_scale = a.row_scale;
   p.col_scale = a.col_scale;
+  p.gu = static_cast<uint16_t*>(a.gu);
+  p.ldgu = a.ldgu;
+  p.h = static_cast<uint16_t*>(a.h);
+  p.ldh = a.ldh;
   p.part = a.ws;
   p.row_tiles = static_cast<i32x4*>(a.ws);
-  if (a.i8) return launch_product<kForward, true>(p, a, stream);
-  if (a.dir == kForward) return launch_product<kForward, false>(p, a, stream);
-  if (a.dir == kGradRows) return launch_product<kGradRows, false>(p, a, stream);
-  return launch_product<kGradWeights, false>(p, a, stream);
+  if (a.type == kInt8) return launch_product<kForward, kInt8>(p, a, stream);
+  if (a.type == kFp8) return launch_product<kForward, kFp8>(p, a, stream);
+  if (a.epilogue == kSwiglu) return launch_product<kForward, kBf16, kSwiglu>(p, a, stream);
+  if (a.epilogue == kSwigluGrad) return launch_product<kGradRows, kBf16, kSwigluGrad>(p, a, stream);
+  if (a.dir == kForward) return launch_product<kForward, kBf16>(p, a, stream);
+  if (a.dir == kGradRows) return launch_product<kGradRows, kBf16>(p, a, stream);
+  return launch_product<kGradWeights, kBf16>(p, a, stream);
 }
 
 }  // namespace eaas

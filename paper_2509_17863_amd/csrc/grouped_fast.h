@@ -48,11 +48,12 @@ __device__ __forceinline__ int swz_across(int row) {
 constexpr int kWayOutLd = 68;  // floats: a pad of 16 bytes against bank conflicts
 constexpr int kWayOutBytes = 32 * kWayOutLd * 4;
 
-template <int DIR, bool I8, int MBW, class Acc>
+template <int DIR, int TYPE, int MBW, class Acc>
 __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTile& t, int split,
                                         int row0, int col0, const Acc (&acc)[MBW][2],
                                         LDS_AS float* buf) {
   constexpr int LD = kWayOutLd;
+  constexpr bool I8 = TYPE == kInt8;
   const int lane = __lane_id();
   const int lrow = lane & 31, khalf = lane >> 5;
   const int cols = columns<DIR>(p);
@@ -182,6 +183,66 @@ __device__ __forceinline__ void way_out(const GroupedParams& p, const GroupedTil
         } else {
           store4<DIR>(p, t.e, row, col, v);
         }
+      }
+    }
+  }
+}
+
+// The same for a product with an epilogue.  kSwiglu: block 0 of a wave holds gate and
+// block 1 up of the 32 columns from col0; kSwigluGrad: 64 columns of dh.  Parts of a split
+// sum are stored as they come, those of kSwiglu at their columns of the matrix.
+template <int DIR, int EPI, int MBW>
+__device__ __forceinline__ void way_out_swiglu(const GroupedParams& p, const GroupedTile& t,
+                                               int split, int row0, int col0,
+                                               const f32x16 (&acc)[MBW][2], LDS_AS float* buf) {
+  constexpr int LD = kWayOutLd;
+  const int lane = __lane_id();
+  const int lrow = lane & 31, khalf = lane >> 5;
+  const int cols = columns<DIR, EPI>(p);
+  if (col0 >= cols) return;
+  // a lane takes eight columns: four or eight lanes to a row
+  constexpr int PER = EPI == kSwiglu ? 4 : 8, ROWS = kWave / PER;
+  const int c = (lane & (PER - 1)) * 8, n = cols - (col0 + c);
+#pragma unroll
+  for (int i = 0; i < MBW; ++i) {
+    LDS_AS float* at = buf + lrow * LD + 4 * khalf;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<LDS_AS f32x4*>(at + j * 32 + 8 * q) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
+                  acc[i][j][4 * q + 3]};
+#pragma unroll
+    for (int s = 0; s < 32 / ROWS; ++s) {
+      const int m = s * ROWS + lane / PER, ri = row0 + i * 32 + m;
+      float a[8], b[8];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const f32x4 x = *reinterpret_cast<const LDS_AS f32x4*>(buf + m * LD + c + 4 * q);
+        const f32x4 y = *reinterpret_cast<const LDS_AS f32x4*>(
+            buf + m * LD + (EPI == kSwiglu ? 32 : 0) + c + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[4 * q + e] = x[e];
+          b[4 * q + e] = y[e];
+        }
+      }
+      if (ri >= t.i_valid || n <= 0) continue;
+      const int row = t.i0 + ri;
+      if (p.splits > 1) {
+        const int wide = columns<DIR>(p);
+        float* o = static_cast<float*>(p.part) + ((size_t)split * p.R + row) * wide + col0 + c;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < n) {
+            o[e] = a[e];
+            if constexpr (EPI == kSwiglu) o[cols + e] = b[e];
+          }
+      } else if constexpr (EPI == kSwiglu) {
+        store_swiglu(p, row, col0 + c, n, a, b);
+      } else {
+        store_swiglu_grad(p, row, col0 + c, n, a);
       }
     }
   }

@@ -102,6 +102,15 @@ struct FfnArgs {
 hipError_t launch_quantize_rows(const uint16_t* x, long long rows, int K, uint8_t* q, float* s,
                                 hipStream_t stream);
 
+// mats matrices [rows,K] (bf16 or fp32, rows ldx apart) -> q e4m3fn and s: a scale for
+// each 128 columns of a row (block_rows 1) or each 128 x 128 block (128).
+hipError_t launch_quantize_blocks(const void* x, bool fp32, long long ldx, long long mats,
+                                  long long rows, int K, int block_rows, uint8_t* q, float* s,
+                                  hipStream_t stream);
+// gu [rows,2I] -> q [rows,I] and s [rows,ceil(I/128)] of silu(gate) * up.
+hipError_t launch_swiglu_fp8(const uint16_t* gu, long long rows, int I, const int32_t* n_rows,
+                             uint8_t* q, float* s, hipStream_t stream);
+
 // fp8 weights [E,N,K] -> the tiled layout the fp8-weight ring kernels read
 // (weight stages contiguous).  I > 0: a gate/up matrix (N = 2I, gate rows then
 // up rows); I == 0: a down matrix.
@@ -147,9 +156,15 @@ hipError_t launch_slot_complete(const eaas_slot* slots, int n_slots, const int32
 
 // Grouped products of an expert's matrix on their own (grouped.h has the frame).
 enum GroupedDir { kForward = 0, kGradRows = 1, kGradWeights = 2 };
+// What the operands are: both bf16, both 8-bit integers or both e4m3 (forward).
+enum GroupedType { kBf16 = 0, kInt8 = 1, kFp8 = 2 };
+// What becomes of the sums: they are the result; h = silu(gate) * up of the two halves of
+// a row (forward); the gradients of gate and up from a row of dh (gradient in the rows).
+enum GroupedEpilogue { kPlain = 0, kSwiglu = 1, kSwigluGrad = 2 };
 struct GroupedArgs {
   int dir;                  // GroupedDir
-  bool i8;                  // 8-bit integers (forward)
+  int type;                 // GroupedType
+  int epilogue;             // GroupedEpilogue
   int R, E, N, K;
   const void* a;            // x | dy | dy, lda elements between rows
   long long lda;
@@ -161,8 +176,14 @@ struct GroupedArgs {
   void* out;
   long long ldo;
   bool out_fp32, accumulate;
-  const float* row_scale;   // 8-bit integers
+  const float* row_scale;   // 8-bit operands
   const float* col_scale;
+  // kSwiglu: out is h, gu (or nullptr) gets the sums; kSwigluGrad: out is dgu, gu is read,
+  // h (or nullptr) is written
+  void* gu;
+  long long ldgu;
+  void* h;
+  long long ldh;
   void* ws;                 // grouped_workspace bytes
 };
 size_t grouped_workspace(const GroupedArgs& a);

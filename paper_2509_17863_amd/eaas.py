@@ -28,7 +28,9 @@ __all__ = [
     "eaas_grouped_workspace_bytes", "alloc_grouped_workspace", "eaas_grouped_matmul",
     "eaas_grouped_matmul_dx", "eaas_grouped_matmul_dw", "eaas_quantize_rows_int8",
     "eaas_grouped_matmul_int8", "eaas_swiglu", "eaas_swiglu_int8", "eaas_swiglu_backward",
-    "eaas_unpermute_combine_backward",
+    "eaas_unpermute_combine_backward", "eaas_quantize_blocks_fp8",
+    "eaas_grouped_fp8_workspace_bytes", "alloc_grouped_fp8_workspace", "eaas_grouped_matmul_fp8",
+    "eaas_grouped_swiglu", "eaas_grouped_swiglu_backward", "eaas_swiglu_fp8",
 ]
 
 EAAS_OK = 0
@@ -47,7 +49,9 @@ EXPORTED = ("eaas_workspace_bytes", "eaas_route_permute", "eaas_expert_ffn_group
             "eaas_grouped_workspace_bytes", "eaas_grouped_matmul", "eaas_grouped_matmul_dx",
             "eaas_grouped_matmul_dw", "eaas_quantize_rows_int8", "eaas_grouped_matmul_int8",
             "eaas_swiglu", "eaas_swiglu_int8", "eaas_swiglu_backward",
-            "eaas_unpermute_combine_backward")
+            "eaas_unpermute_combine_backward", "eaas_quantize_blocks_fp8",
+            "eaas_grouped_fp8_workspace_bytes", "eaas_grouped_matmul_fp8", "eaas_grouped_swiglu",
+            "eaas_grouped_swiglu_backward", "eaas_swiglu_fp8")
 
 _DEFAULT_LIB = Path(__file__).resolve().parent / "libeaas.so"
 _LIB_PATH = _DEFAULT_LIB
@@ -135,9 +139,21 @@ def _bind(L: ctypes.CDLL) -> ctypes.CDLL:
     L.eaas_swiglu_int8.argtypes = [vp, i64, ctypes.c_int32, vp, vp, vp, vp]
     L.eaas_swiglu_backward.argtypes = [vp, vp, i64, ctypes.c_int32, vp, vp, vp]
     L.eaas_unpermute_combine_backward.argtypes = [sp, vp, i32, vp, rp, vp, vp, vp, vp]
+    L.eaas_quantize_blocks_fp8.argtypes = [vp, i32, i64, ctypes.c_int32, i64, ctypes.c_int32,
+                                           ctypes.c_int32, vp, vp, vp]
+    L.eaas_grouped_fp8_workspace_bytes.argtypes = [gp]
+    L.eaas_grouped_fp8_workspace_bytes.restype = sz
+    L.eaas_grouped_matmul_fp8.argtypes = L.eaas_grouped_matmul_int8.argtypes
+    L.eaas_grouped_swiglu.argtypes = [gp, vp, i64, vp, ctypes.c_int32, vp, vp, vp, i64, vp, i64,
+                                      vp, sz, vp]
+    L.eaas_grouped_swiglu_backward.argtypes = [gp, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, vp,
+                                               sz, vp]
+    L.eaas_swiglu_fp8.argtypes = L.eaas_swiglu_int8.argtypes
     for name in ("eaas_grouped_matmul", "eaas_grouped_matmul_dx", "eaas_grouped_matmul_dw",
                  "eaas_grouped_matmul_int8", "eaas_quantize_rows_int8", "eaas_swiglu",
-                 "eaas_swiglu_int8", "eaas_swiglu_backward", "eaas_unpermute_combine_backward"):
+                 "eaas_swiglu_int8", "eaas_swiglu_backward", "eaas_unpermute_combine_backward",
+                 "eaas_quantize_blocks_fp8", "eaas_grouped_matmul_fp8", "eaas_grouped_swiglu",
+                 "eaas_grouped_swiglu_backward", "eaas_swiglu_fp8"):
         getattr(L, name).restype = i32
     L.eaas_status_string.argtypes = [i32]
     L.eaas_status_string.restype = ctypes.c_char_p
@@ -514,12 +530,13 @@ _GROUPED_KERNELS = ("any", "few", "large")
 
 def _grouped_plan(product: str, R, E, N, K, in16: bool) -> tuple[str, int, int]:
     """(kernel, rows of its tiles, parts of the sum) of the product "forward", "dx",
-    "dw" or "int8": the library's own choice, asked on the host, for tests and
-    measurements.  in16: sizes, strides and bases are multiples of 16 bytes."""
+    "dw", "int8", "fp8", "swiglu" or "swiglu_backward": the library's own choice, asked
+    on the host, for tests and measurements.  in16: sizes, strides and bases are
+    multiples of 16 bytes."""
     s = _group_shape(R, E, N, K)
-    d = ("forward", "dx", "dw").index("forward" if product == "int8" else product)
-    r = int(lib().eaas_internal_grouped_plan(ctypes.byref(s), d, int(product == "int8"),
-                                             int(in16)))
+    d, kind = {"forward": (0, 0), "dx": (1, 0), "dw": (2, 0), "int8": (0, 1), "fp8": (0, 2),
+               "swiglu": (0, 3), "swiglu_backward": (1, 3)}[product]
+    r = int(lib().eaas_internal_grouped_plan(ctypes.byref(s), d, kind, int(in16)))
     if r < 0:
         raise EaasError(-2, "eaas_internal_grouped_plan")
     return _GROUPED_KERNELS[r & 3], (r & 4095) >> 2, r >> 12
@@ -621,6 +638,117 @@ def eaas_grouped_matmul_int8(xq: torch.Tensor, xs: torch.Tensor, offsets: torch.
         _OUT[y.dtype], _p(ws), ws.numel(), _stream(stream)), "eaas_grouped_matmul_int8")
 
 
+def _blocks(n: int) -> int:
+    return (n + 127) // 128
+
+
+_CODES = (torch.uint8, torch.float8_e4m3fn)
+
+
+def _codes(t: torch.Tensor, *shape) -> int:
+    if t.dtype not in _CODES:
+        raise ValueError(f"e4m3 codes are uint8 or float8_e4m3fn, got {t.dtype}")
+    return _dense(t, t.dtype, *shape)
+
+
+def eaas_quantize_blocks_fp8(x: torch.Tensor, q: torch.Tensor, s: torch.Tensor,
+                             stream=None) -> None:
+    """x bf16 or fp32 -> q, e4m3 codes of its shape (uint8 or float8_e4m3fn), and fp32
+    scales: of rows x [rows, K] (which may be cut out of a wider array) one for each 128
+    columns, s [rows, ceil(K/128)]; of weights x [E, N, K] one for each block of 128 x
+    128, s [E, ceil(N/128), ceil(K/128)]."""
+    K = x.shape[-1]
+    if x.dtype not in _OUT:
+        raise ValueError(f"x must be bf16 or fp32, got {x.dtype}")
+    if x.dim() == 3:
+        E, N, _ = x.shape
+        xp, ldx, mats, rows, per = _p(x), K, E, N, 128
+        sp = _dense(s, torch.float32, E, _blocks(N), _blocks(K))
+    else:
+        xp, ldx = _rows(x, K)
+        mats, rows, per = 1, x.shape[0], 1
+        sp = _dense(s, torch.float32, rows, _blocks(K))
+    _check(lib().eaas_quantize_blocks_fp8(xp, _OUT[x.dtype], ldx, mats, rows, K, per,
+                                          _codes(q, *x.shape), sp, _stream(stream)),
+           "eaas_quantize_blocks_fp8")
+
+
+def eaas_grouped_fp8_workspace_bytes(R, E, N, K) -> int:
+    return int(lib().eaas_grouped_fp8_workspace_bytes(ctypes.byref(_group_shape(R, E, N, K))))
+
+
+def alloc_grouped_fp8_workspace(R, E, N, K, device="cuda") -> torch.Tensor:
+    """Workspace of eaas_grouped_matmul_fp8 for R rows with E matrices [N, K]."""
+    n = eaas_grouped_fp8_workspace_bytes(R, E, N, K)
+    if n == 0:
+        raise EaasError(-2, "eaas_grouped_fp8_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def eaas_grouped_matmul_fp8(xq: torch.Tensor, xs: torch.Tensor, offsets: torch.Tensor,
+                            wq: torch.Tensor, wscale: torch.Tensor, y: torch.Tensor,
+                            ws: torch.Tensor, perm=None, k: int = 1, stream=None) -> None:
+    """The product of e4m3 codes with scales for each block of 128
+    (eaas_quantize_blocks_fp8): xq [R, K] (or the tokens, with perm) with xs [.., K/128],
+    wq [E, N, K] with wscale [E, N/128, K/128] (quotients rounded up), y [R, N] bf16 or
+    fp32."""
+    E, N, K = wq.shape
+    R = y.shape[0]
+    yp, ldy = _rows(y, N, (torch.bfloat16, torch.float32))
+    pp, kk = _gather(xq, R, perm, k)
+    s = _group_shape(R, E, N, K)
+    _check(lib().eaas_grouped_matmul_fp8(
+        ctypes.byref(s), _codes(xq, xq.shape[0], K),
+        _dense(xs, torch.float32, xq.shape[0], _blocks(K)), pp, kk,
+        _dense(offsets, torch.int32, E + 1), _codes(wq, E, N, K),
+        _dense(wscale, torch.float32, E, _blocks(N), _blocks(K)), yp, ldy, _OUT[y.dtype], _p(ws),
+        ws.numel(), _stream(stream)), "eaas_grouped_matmul_fp8")
+
+
+def eaas_grouped_swiglu(x: torch.Tensor, offsets: torch.Tensor, w: torch.Tensor, h: torch.Tensor,
+                        ws: torch.Tensor, gu=None, perm=None, k: int = 1, stream=None) -> None:
+    """h[r] = silu(w[e,:I] @ x[r]) * (w[e,I:] @ x[r]): x as in eaas_grouped_matmul, w
+    [E, 2I, K] bf16, h [R, I] bf16; gu [R, 2I] bf16, if given, gets the two products
+    (for the backward pass).  Workspace: alloc_grouped_workspace(R, E, 2I, K)."""
+    E, N, K = w.shape
+    if N % 2:
+        raise ValueError("w holds the gate rows, then as many up rows")
+    R = h.shape[0]
+    xp, ldx = _rows(x, K, torch.bfloat16)
+    hp, ldh = _rows(h, N // 2, torch.bfloat16)
+    pp, kk = _gather(x, R, perm, k)
+    gp, ldgu = (None, N) if gu is None else _rows(gu, N, torch.bfloat16)
+    if gu is not None and gu.shape[0] != R:
+        raise ValueError(f"gu has {gu.shape[0]} rows, h {R}")
+    s = _group_shape(R, E, N, K)
+    _check(lib().eaas_grouped_swiglu(
+        ctypes.byref(s), xp, ldx, pp, kk, _dense(offsets, torch.int32, E + 1),
+        _dense(w, torch.bfloat16, E, N, K), hp, ldh, gp, ldgu, _p(ws), ws.numel(),
+        _stream(stream)), "eaas_grouped_swiglu")
+
+
+def eaas_grouped_swiglu_backward(dy: torch.Tensor, offsets: torch.Tensor, w: torch.Tensor,
+                                 gu: torch.Tensor, dgu: torch.Tensor, ws: torch.Tensor, h=None,
+                                 stream=None) -> None:
+    """From dy [R, N] bf16, the gradient of w[e] @ h[r] with w [E, N, I] bf16, and gu
+    [R, 2I] bf16: dgu [R, 2I] bf16 (dgate, then dup; may be gu itself) and, if given, h
+    [R, I] bf16 again.  Workspace: alloc_grouped_workspace(R, E, N, I)."""
+    E, N, I = w.shape
+    R = dgu.shape[0]
+    for name, t in (("dy", dy), ("gu", gu), ("h", h)):
+        if t is not None and t.shape[0] != R:
+            raise ValueError(f"{name} has {t.shape[0]} rows, dgu {R}")
+    dyp, lddy = _rows(dy, N, torch.bfloat16)
+    gp, ldgu = _rows(gu, 2 * I, torch.bfloat16)
+    dp, lddgu = _rows(dgu, 2 * I, torch.bfloat16)
+    hp, ldh = (None, I) if h is None else _rows(h, I, torch.bfloat16)
+    s = _group_shape(R, E, N, I)
+    _check(lib().eaas_grouped_swiglu_backward(
+        ctypes.byref(s), dyp, lddy, _dense(offsets, torch.int32, E + 1),
+        _dense(w, torch.bfloat16, E, N, I), gp, ldgu, dp, lddgu, hp, ldh, _p(ws), ws.numel(),
+        _stream(stream)), "eaas_grouped_swiglu_backward")
+
+
 def _half(gu: torch.Tensor) -> tuple[int, int]:
     rows, two = gu.shape
     if two % 2:
@@ -650,6 +778,16 @@ def eaas_swiglu_int8(gu: torch.Tensor, q: torch.Tensor, s: torch.Tensor, n_rows=
                                   _count(n_rows), _dense(q, torch.int8, rows, I),
                                   _dense(s, torch.float32, rows), _stream(stream)),
            "eaas_swiglu_int8")
+
+
+def eaas_swiglu_fp8(gu: torch.Tensor, q: torch.Tensor, s: torch.Tensor, n_rows=None,
+                    stream=None) -> None:
+    """The same as e4m3 codes q [rows, I] with a scale for each 128 columns, s [rows,
+    ceil(I/128)] fp32."""
+    rows, I = _half(gu)
+    _check(lib().eaas_swiglu_fp8(_dense(gu, torch.bfloat16, rows, 2 * I), rows, I, _count(n_rows),
+                                 _codes(q, rows, I), _dense(s, torch.float32, rows, _blocks(I)),
+                                 _stream(stream)), "eaas_swiglu_fp8")
 
 
 def eaas_swiglu_backward(gu: torch.Tensor, dh: torch.Tensor, dgu: torch.Tensor, n_rows=None,
