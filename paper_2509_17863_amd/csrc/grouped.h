@@ -282,8 +282,13 @@ __device__ __forceinline__ void store_swiglu_grad(const GroupedParams& p, size_t
 template <int DIR, bool I8>
 hipError_t launch_grouped_pp(const GroupedParams& p, long long tiles, hipStream_t stream);
 
+// grouped_swiglu.hip: the same with an epilogue.
+hipError_t launch_grouped_swiglu_pp(const GroupedParams& p, long long tiles, hipStream_t stream);
+hipError_t launch_grouped_swiglu_grad_pp(const GroupedParams& p, long long tiles,
+                                         hipStream_t stream);
+
 // grouped_few.hip: tiles of `rows` (16, 32 or 64) x 64 under the same condition.
-template <int DIR, bool I8>
+template <int DIR, int TYPE, int EPI>
 hipError_t launch_grouped_few(const GroupedParams& p, int rows, long long tiles,
                               hipStream_t stream);
 

@@ -500,10 +500,11 @@ GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   GroupedPlan any{kAny, kBI, kBJ, 1};
   double t_any;
   any.splits = best_parts(steps, out, [&](int s) { return any_us(tiles, steps, s); }, &t_any);
-  if (!in16 || a.type == kFp8 || a.epilogue != kPlain) return any;
+  if (!in16) return any;
   if (a.dir == kGradWeights) return rows >= 128 && large >= 48 ? on_large : any;
+  const bool has_large = a.type != kFp8;
   const int some = a.dir == kForward && a.type == kBf16 ? 48 : 16;
-  if (rows >= some && large >= 192 && steps >= 4) return on_large;
+  if (has_large && rows >= some && large >= 192 && steps >= 4) return on_large;
   GroupedPlan few{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};
   const double cells = (double)out_tiles(a, few.bi, few.bj);
   double t_few;
@@ -511,7 +512,7 @@ GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
                           &t_few);
   if (rows <= 24 && steps >= 4) return few;
   const double t_large = large_us((double)large, steps);
-  return t_large < std::min(t_any, t_few) ? on_large : t_few < t_any ? few : any;
+  return has_large && t_large < std::min(t_any, t_few) ? on_large : t_few < t_any ? few : any;
 }
 
 // Workspace: the parts of a split sum, or the large tiles' table of row tiles.
@@ -533,9 +534,11 @@ hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t str
   if (g.kernel == kLarge) {
     if constexpr (EPI == kPlain && TYPE != kFp8)
       e = launch_grouped_pp<DIR, TYPE == kInt8>(p, tiles, stream);
+    if constexpr (EPI == kSwiglu) e = launch_grouped_swiglu_pp(p, tiles, stream);
+    if constexpr (EPI == kSwigluGrad) e = launch_grouped_swiglu_grad_pp(p, tiles, stream);
   } else if (g.kernel == kFew) {
-    if constexpr (DIR != kGradWeights && EPI == kPlain && TYPE != kFp8)
-      e = launch_grouped_few<DIR, TYPE == kInt8>(p, g.bi, tiles, stream);
+    if constexpr (DIR != kGradWeights)
+      e = launch_grouped_few<DIR, TYPE, EPI>(p, g.bi, tiles, stream);
   } else {
     hipLaunchKernelGGL((grouped_any_kernel<DIR, TYPE, EPI>), tile_grid(tiles, p.splits),
                        dim3(kThreads), 0, stream, p);

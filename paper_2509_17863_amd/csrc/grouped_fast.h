@@ -17,6 +17,12 @@ __device__ __forceinline__ void load_lds16(const i32x4& rsrc, uint32_t voff, uin
                :: "v"(voff), "s"(rsrc), "s"(lds) : "memory");
 }
 
+// The same with 4 bytes a lane, landing at lds + 4 * l.
+__device__ __forceinline__ void load_lds4(const i32x4& rsrc, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds"
+               :: "v"(voff), "s"(rsrc), "s"(lds) : "memory");
+}
+
 // Raw buffer descriptor of `bytes` bytes from `base` (both wave-uniform).
 __device__ __forceinline__ i32x4 descriptor(const char* base, uint32_t bytes) {
   const uint64_t v = reinterpret_cast<uint64_t>(base);

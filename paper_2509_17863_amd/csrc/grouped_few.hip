@@ -12,6 +12,10 @@
 // to a CU for 16 rows; three stages for 32 and two for 64, one workgroup: 96 to 150
 // KiB in flight on a CU, several times what the memory's latency asks for.)
 //
+// kSwiglu: the 64 weight rows are 32 gate rows and the up rows of the same columns.  kFp8:
+// a tile of the sum is one block of scales; the rows' scales travel in the stage, and codes
+// go to bf16 as they are read (grouped.hip, fp8_block), which memory leaves time for.
+//
 // Measured, reading the weights once: 4 rows of each of 128 experts, 2048 x 768:
 // forward 76 us (5.3 TB/s), dx 71 (5.6); one token, 8 of 32
 // experts, 4096 x 7168 in 8-bit integers: 37 us (6.4); 8 tokens on 128 experts, 1536 x
@@ -29,24 +33,27 @@ constexpr int kWBytes = kJ * 128;  // weights of a stage
 // transposing load (16 lanes: 4 rows x 32 bytes).
 __device__ __forceinline__ int swz_sum(int row) { return (((row & 3) ^ ((row >> 3) & 1)) << 1); }
 
-template <int DIR, bool I8, int MB, int STAGES>
+template <int DIR, int TYPE, int EPI, int MB, int STAGES>
 __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) {
   constexpr bool B_ACROSS = DIR == kGradRows;
-  constexpr int ESZ = I8 ? 1 : 2, SUM = 128 / ESZ;
+  constexpr bool I8 = TYPE == kInt8, FP8 = TYPE == kFp8;
+  constexpr int ESZ = TYPE == kBf16 ? 2 : 1, SUM = 128 / ESZ;
   constexpr int BI = 16 * MB, NB = kJ / 16;
-  constexpr int kXBytes = BI * 128, kStage = kWBytes + kXBytes;
-  constexpr int W_INST = kWBytes / 1024, X_INST = kXBytes / 1024, INST = W_INST + X_INST;
+  constexpr int kOutJ = EPI == kSwiglu ? kJ / 2 : kJ;  // columns of a result tile
+  constexpr int kXBytes = BI * 128, kSBytes = FP8 ? 256 : 0, kStage = kWBytes + kXBytes + kSBytes;
+  constexpr int W_INST = kWBytes / 1024, X_INST = kXBytes / 1024;
+  constexpr int INST = W_INST + X_INST + (FP8 ? 1 : 0);
   constexpr int LD = kJ + 4;
   constexpr int kRing = kWaves * STAGES * kStage, kParts = kWaves * BI * LD * 4;
   __shared__ __attribute__((aligned(1024))) char smem_raw[kRing > kParts ? kRing : kParts];
   GroupedTile t;
-  if (!find_tile<DIR, BI, kJ, kThreads>(p, reinterpret_cast<int*>(smem_raw), t)) return;
+  if (!find_tile<DIR, BI, kOutJ, kThreads, EPI>(p, reinterpret_cast<int*>(smem_raw), t)) return;
 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
   const uint32_t lds0 =
       __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem_raw) + wave * STAGES * kStage;
-  const int cols = columns<DIR>(p);
+  const int cols = columns<DIR, EPI>(p);
   const int sum_end = DIR == kForward ? p.K : p.N;
   const int tiles = ceil_div(sum_end, SUM);
   const int parts = p.splits * kWaves, part = blockIdx.y * kWaves + wave;
@@ -76,9 +83,23 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
                  (B_ACROSS ? t.j0 * ESZ + ((c8 ^ swz_sum(row)) * 16) : (c8 ^ swz_along(row)) * 16);
   }
   const char* w_base = B_ACROSS ? w : w + t.j0 * b_row;
-  const uint32_t w_bytes = (uint32_t)(min(kJ, cols - t.j0) * b_row);
+  const uint32_t w_bytes = (uint32_t)(min(kOutJ, cols - t.j0) * b_row);
   const int chunks = ceil_div(sum_end * ESZ, 16);  // of the sum
 
+  // kFp8: a lane's row of x has its scales there, and the columns, which lie in one block
+  // of 128, have theirs at col_scale
+  const int kb = FP8 ? ceil_div(p.K, 128) : 0;
+  const char* s_base = nullptr;
+  uint32_t s_bytes = 0, s_off = 0;
+  const CONST_AS float* col_scale = nullptr;
+  if constexpr (FP8) {
+    const int row = min(lane, t.i_valid - 1);
+    s_base = reinterpret_cast<const char*>(p.row_scale + (gather ? 0 : (size_t)t.i0 * kb));
+    s_bytes = (uint32_t)((gather ? p.R / p.k : t.i_valid) * 4LL * kb);
+    s_off = (uint32_t)((gather ? source_row(p, t.i0 + row) : row) * 4LL * kb);
+    col_scale = (const CONST_AS float*)(p.col_scale +
+                                        ((size_t)t.e * ceil_div(p.N, 128) + t.j0 / 128) * kb);
+  }
   auto issue = [&](int kt) {
     const int at = first + kt;
     const uint32_t dst = lds0 + (kt % STAGES) * kStage;
@@ -93,16 +114,26 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
       for (int q = 0; q < W_INST; ++q)
         load_lds16(d, w_off[q & 1] + (uint32_t)((q & ~1) * 8 * b_row), dst + q * 1024);
     } else {
-      const i32x4 d = descriptor(w_base + (size_t)at * 128, w_bytes - (uint32_t)at * 128);
+      const char* from = w_base + (size_t)at * 128;
+      const uint32_t bytes = w_bytes - (uint32_t)at * 128;
+      // (kSwiglu: gate rows, then up rows)
+      constexpr int HALF = EPI == kSwiglu ? W_INST / 2 : W_INST;
 #pragma unroll
-      for (int q = 0; q < W_INST; ++q)
-        load_lds16(d, (q & 1 ? odd : even) ? w_off[q & 1] + (uint32_t)((q & ~1) * 8 * b_row)
-                                           : kNowhere, dst + q * 1024);
+      for (int first_q = 0; first_q < W_INST; first_q += HALF) {
+        const i32x4 d = descriptor(from + (first_q ? cols * b_row : 0), bytes);
+#pragma unroll
+        for (int q = 0; q < HALF; ++q)
+          load_lds16(d, (q & 1 ? odd : even) ? w_off[q & 1] + (uint32_t)((q & ~1) * 8 * b_row)
+                                             : kNowhere, dst + (first_q + q) * 1024);
+      }
     }
     const i32x4 d = descriptor(x_base + (size_t)at * 128, x_bytes - (uint32_t)at * 128);
 #pragma unroll
     for (int q = 0; q < X_INST; ++q)
       load_lds16(d, (q & 1 ? odd : even) ? x_off[q] : kNowhere, dst + kWBytes + q * 1024);
+    if constexpr (FP8)
+      load_lds4(descriptor(s_base + (size_t)at * 4, s_bytes - (uint32_t)at * 4), s_off,
+                dst + kWBytes + kXBytes);
   };
 
   // fragments of v_mfma_*_16x16: lane l holds row or column l % 16 and 16 bytes of
@@ -115,7 +146,14 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[i][j] = Acc{};
   const LDS_AS char* ring = (const LDS_AS char*)smem_raw + wave * STAGES * kStage;
-  auto multiply = [&](const LDS_AS char* stage) {
+  auto multiply = [&](const LDS_AS char* stage, float col) {
+    f32x4 part[FP8 ? MB : 1][FP8 ? NB : 1];
+    if constexpr (FP8) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) part[i][j] = f32x4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       u32x4 fw[NB], fx[MB];
@@ -145,6 +183,22 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
         fx[i] = *reinterpret_cast<const LDS_AS u32x4*>(stage + kWBytes + row * 128 +
                                                        ((chunk ^ swz_along(row)) << 4));
       }
+      if constexpr (FP8) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          bf16x8 bx[MB];
+#pragma unroll
+          for (int i = 0; i < MB; ++i) bx[i] = fp8x8_to_bf16(u32x2{fx[i][2 * h], fx[i][2 * h + 1]});
+#pragma unroll
+          for (int j = 0; j < NB; ++j) {
+            const bf16x8 bw = fp8x8_to_bf16(u32x2{fw[j][2 * h], fw[j][2 * h + 1]});
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+              part[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw, bx[i], part[i][j], 0, 0, 0);
+          }
+        }
+        continue;
+      }
 #pragma unroll
       for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -159,17 +213,31 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
                 0, 0);
         }
     }
+    if constexpr (FP8) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) {
+        const float f = col * *reinterpret_cast<const LDS_AS float*>(stage + kWBytes + kXBytes +
+                                                                     (i * 16 + l16) * 4);
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) acc[i][j][v] = fmaf(part[i][j][v], f, acc[i][j][v]);
+      }
+    }
   };
 
 #pragma unroll
   for (int s = 0; s < STAGES; ++s)
     if (s < nk) issue(s);
+  float col = FP8 && nk > 0 ? col_scale[first] : 0.0f;
   for (int kt = 0; kt < nk; ++kt) {
+    const float next = FP8 ? col_scale[first + min(kt + 1, nk - 1)] : 0.0f;
     // (past the last full ring the count is not known here: wait for all)
     if (kt + STAGES <= nk) wait_vmcnt<(STAGES - 1) * INST>();
     else wait_vmcnt<0>();
     asm volatile("" ::: "memory");
-    multiply(ring + (kt % STAGES) * kStage);
+    multiply(ring + (kt % STAGES) * kStage, col);
+    col = next;
     // the stage is read: it may be filled again
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     if (kt + STAGES < nk) issue(kt + STAGES);
@@ -185,6 +253,46 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
       *reinterpret_cast<LDS_AS Acc*>(sums + ((wave * BI + i * 16 + l16) * LD + j * 16 + 4 * g) * 4) =
           acc[i][j];
   __syncthreads();
+  if constexpr (EPI != kPlain) {
+    // eight columns of the result a thread
+    constexpr int PER = kOutJ / 8;
+    for (int u = threadIdx.x; u < BI * PER; u += kThreads) {
+      const int ri = u / PER, c = (u % PER) * 8, col0 = t.j0 + c, n = cols - col0;
+      if (ri >= t.i_valid || n <= 0) continue;
+      const int row = t.i0 + ri;
+      float a[8] = {}, b[8] = {};
+#pragma unroll
+      for (int s = 0; s < kWaves; ++s)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const LDS_AS char* from = sums + ((s * BI + ri) * LD + c + 4 * q) * 4;
+          const f32x4 x = *reinterpret_cast<const LDS_AS f32x4*>(from);
+          f32x4 y = x;
+          if constexpr (EPI == kSwiglu)
+            y = *reinterpret_cast<const LDS_AS f32x4*>(from + kOutJ * 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            a[4 * q + e] += x[e];
+            b[4 * q + e] += y[e];
+          }
+        }
+      if (p.splits > 1) {
+        const int wide = columns<DIR>(p);
+        float* o = static_cast<float*>(p.part) + ((size_t)blockIdx.y * p.R + row) * wide + col0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < n) {
+            o[e] = a[e];
+            if constexpr (EPI == kSwiglu) o[cols + e] = b[e];
+          }
+      } else if constexpr (EPI == kSwiglu) {
+        store_swiglu(p, row, col0, n, a, b);
+      } else {
+        store_swiglu_grad(p, row, col0, n, a);
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int u = 0; u < MB; ++u) {
     const int ri = u * 16 + (int)threadIdx.x / 16, c = (threadIdx.x & 15) * 4;
@@ -208,26 +316,30 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
   }
 }
 
-template <int DIR, bool I8, int MB, int STAGES>
+template <int DIR, int TYPE, int EPI, int MB, int STAGES>
 hipError_t launch(const GroupedParams& p, long long tiles, hipStream_t stream) {
-  hipLaunchKernelGGL((grouped_few_kernel<DIR, I8, MB, STAGES>), tile_grid(tiles, p.splits),
+  hipLaunchKernelGGL((grouped_few_kernel<DIR, TYPE, EPI, MB, STAGES>), tile_grid(tiles, p.splits),
                      dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-template <int DIR, bool I8>
+template <int DIR, int TYPE, int EPI>
 hipError_t launch_grouped_few(const GroupedParams& p, int rows, long long tiles,
                               hipStream_t stream) {
   if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
-  if (rows == 16) return launch<DIR, I8, 1, 2>(p, tiles, stream);
-  if (rows == 32) return launch<DIR, I8, 2, 3>(p, tiles, stream);
-  return launch<DIR, I8, 4, 2>(p, tiles, stream);
+  // (kFp8: with the rows' scales two workgroups of 16 rows no longer fit a CU)
+  if (rows == 16) return launch<DIR, TYPE, EPI, 1, TYPE == kFp8 ? 3 : 2>(p, tiles, stream);
+  if (rows == 32) return launch<DIR, TYPE, EPI, 2, 3>(p, tiles, stream);
+  return launch<DIR, TYPE, EPI, 4, 2>(p, tiles, stream);
 }
 
-template hipError_t launch_grouped_few<kForward, false>(const GroupedParams&, int, long long, hipStream_t);
-template hipError_t launch_grouped_few<kForward, true>(const GroupedParams&, int, long long, hipStream_t);
-template hipError_t launch_grouped_few<kGradRows, false>(const GroupedParams&, int, long long, hipStream_t);
+template hipError_t launch_grouped_few<kForward, kBf16, kPlain>(const GroupedParams&, int, long long, hipStream_t);
+template hipError_t launch_grouped_few<kForward, kInt8, kPlain>(const GroupedParams&, int, long long, hipStream_t);
+template hipError_t launch_grouped_few<kForward, kFp8, kPlain>(const GroupedParams&, int, long long, hipStream_t);
+template hipError_t launch_grouped_few<kForward, kBf16, kSwiglu>(const GroupedParams&, int, long long, hipStream_t);
+template hipError_t launch_grouped_few<kGradRows, kBf16, kPlain>(const GroupedParams&, int, long long, hipStream_t);
+template hipError_t launch_grouped_few<kGradRows, kBf16, kSwigluGrad>(const GroupedParams&, int, long long, hipStream_t);
 
 }  // namespace eaas
