@@ -17,7 +17,8 @@ CSRC = PKG / "csrc"
 BUILD = PKG / "_build"
 LIB = PKG / "libeaas.so"
 SOURCES = ["route.hip", "gemm.hip", "gemm_stream.hip", "combine.hip", "segments.hip", "quant.hip", "eaas_api.hip",
-           "grouped.hip", "grouped_fast.hip", "grouped_swiglu.hip", "grouped_few.hip", "activation.hip", "grouped_api.hip"]
+           "grouped.hip", "grouped_fast.hip", "grouped_swiglu.hip", "grouped_fp8.hip",
+           "grouped_few.hip", "activation.hip", "grouped_api.hip"]
 # scheduler variants of the grouped GEMMs: library name -> EAAS_SCHEDULER
 SCHEDULER_VARIANTS = {"scan_all": 1, "walk_all": 2}
 ARCH = "gfx950"

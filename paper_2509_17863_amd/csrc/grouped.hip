@@ -502,7 +502,7 @@ GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   any.splits = best_parts(steps, out, [&](int s) { return any_us(tiles, steps, s); }, &t_any);
   if (!in16) return any;
   if (a.dir == kGradWeights) return rows >= 128 && large >= 48 ? on_large : any;
-  const bool has_large = a.type != kFp8;
+  const bool has_large = a.type != kFp8 || !a.out_fp32;
   const int some = a.dir == kForward && a.type == kBf16 ? 48 : 16;
   if (has_large && rows >= some && large >= 192 && steps >= 4) return on_large;
   GroupedPlan few{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};
@@ -534,6 +534,7 @@ hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t str
   if (g.kernel == kLarge) {
     if constexpr (EPI == kPlain && TYPE != kFp8)
       e = launch_grouped_pp<DIR, TYPE == kInt8>(p, tiles, stream);
+    if constexpr (TYPE == kFp8) e = launch_grouped_fp8_pp(p, tiles, stream);
     if constexpr (EPI == kSwiglu) e = launch_grouped_swiglu_pp(p, tiles, stream);
     if constexpr (EPI == kSwigluGrad) e = launch_grouped_swiglu_grad_pp(p, tiles, stream);
   } else if (g.kernel == kFew) {

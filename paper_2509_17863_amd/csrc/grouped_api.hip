@@ -148,7 +148,12 @@ size_t eaas_grouped_workspace_bytes(const eaas_group_shape* s) {
 
 size_t eaas_grouped_fp8_workspace_bytes(const eaas_group_shape* s) {
   if (check_group(s) != EAAS_OK) return 0;
-  const size_t n = std::max<size_t>(256, grouped_workspace_most(args_of(s, kForward, kFp8)));
+  size_t n = 256;
+  GroupedArgs a = args_of(s, kForward, kFp8);
+  for (const bool fp32 : {false, true}) {
+    a.out_fp32 = fp32;
+    n = std::max(n, grouped_workspace_most(a));
+  }
   return (n + 255) / 256 * 256;
 }
 
@@ -440,11 +445,11 @@ int eaas_unpermute_combine_backward(const eaas_shape* s, const void* dout, int d
 
 // Not part of the ABI: the kernel that a product takes, for tests and measurements
 // (grouped_plan_code), or -1 for what the library rejects.  dir: 0 forward, 1 gradient
-// in the rows, 2 in the weights; type: 0 bf16, 1 8-bit integers, 2 e4m3 (forward); 3 the
-// product in dir with its epilogue (kSwiglu, kSwigluGrad); in16: sizes, strides and bases
-// in multiples of 16 bytes.
+// in the rows, 2 in the weights; type: 0 bf16, 1 8-bit integers, 2 e4m3 with bf16 results
+// (forward); 3 the product in dir with its epilogue (kSwiglu, kSwigluGrad); 4 e4m3 with
+// fp32 results; in16: sizes, strides and bases in multiples of 16 bytes.
 int eaas_internal_grouped_plan(const eaas_group_shape* s, int dir, int type, int in16) {
-  if (check_group(s) != EAAS_OK || dir < kForward || dir > kGradWeights || type < 0 || type > 3)
+  if (check_group(s) != EAAS_OK || dir < kForward || dir > kGradWeights || type < 0 || type > 4)
     return -1;
   if (type == 3) {
     if (dir == kGradWeights || (dir == kForward && s->N % 2)) return -1;
@@ -452,7 +457,9 @@ int eaas_internal_grouped_plan(const eaas_group_shape* s, int dir, int type, int
                              in16 != 0);
   }
   if (type != kBf16 && dir != kForward) return -1;
-  return grouped_plan_code(args_of(s, dir, type), in16 != 0);
+  GroupedArgs a = args_of(s, dir, type == 4 ? kFp8 : type);
+  a.out_fp32 = type == 4;
+  return grouped_plan_code(a, in16 != 0);
 }
 
 }  // extern "C"

@@ -1,0 +1,291 @@
+// The grouped product of block-scaled e4m3 codes on large tiles, with bf16 results
+// (grouped.h states the product; sizes and addresses in multiples of 16 bytes).
+//
+// v_mfma_f32_16x16x128_f8f6f4 takes a whole block of 128 elements of the sum, one block of
+// scales of both operands, in one instruction; its sums are added to the accumulators times
+// the product of the row's scale and the columns'.  What the instruction keeps is less than
+// fp32: it adds eight products at a time, each first rounded to a multiple of 2^-13 of the
+// power of two under the largest (so by at most 2^-14 of that; whole blocks of eight are
+// then added in fp32).  On normal data that is 1.3e-5 of the results' norm, a three
+// hundredth of what rounding them to bf16 takes, so bf16 results come from here, at twice
+// the rate of bf16 operands; fp32 results come from the kernels that convert codes to bf16,
+// whose products and sums lose nothing (grouped.hip, fp8_block).
+//
+// The loop is that of grouped_pp.h: eight waves compute 256 x 256 results, the two groups of
+// four alternate between reading a tile's fragments and multiplying, one phase apart:
+//   group 0, phase 2t:   M(t): load A tile t+1 and its rows' scales, fragments of tile t
+//   group 0, phase 2t+1: C(t), then wait until A tile t+1 has landed
+//   group 1, phase 2t+1: M(t): fragments of tile t, wait until B tile t+1 has landed
+//   group 1, phase 2t+2: C(t), with the loads of B tile t+2 among its first instructions
+// Both operands have two LDS stages: group 1 loads in its C phase, when the stage that tile
+// t had is free, so no third one is needed, and the scales and the way out have room.
+#include "grouped_pp.h"
+
+namespace eaas {
+namespace {
+
+#define INLINE __attribute__((always_inline))
+
+constexpr int kScales = 4 * kStage;            // LDS: rows' scales, two stages of 1 KiB
+constexpr int kOffsets = kScales + 2 * 1024;   // gathered rows' offsets
+constexpr int kOut = kOffsets + 1024;          // 2 KiB for each wave's way out
+constexpr int kFp8Lds = kOut + 8 * 2048;
+
+// A wave's 128 x 64 results, 16 rows at a time through 2 KiB of its own: acc[i][j][v] is
+// row i*16 + lane % 16, column j*16 + 4*(lane/16) + v.
+template <class F>
+__device__ __forceinline__ void store_fp8_results(const GroupedParams& p, const GroupedTile& t,
+                                                  int row0, int col0, const f32x4 (&acc)[8][4],
+                                                  LDS_AS char* buf, F before_stores) {
+  const int lane = __lane_id();
+  const int l16 = lane & 15, kq = lane >> 4, m8 = lane >> 3, c8 = lane & 7;
+  const int col = col0 + c8 * 8, n = p.N - col;
+  before_stores();
+  if (row0 >= t.i_valid || col0 >= p.N) return;
+  uint16_t* out = static_cast<uint16_t*>(p.out);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<LDS_AS u32x2*>(buf + l16 * 128 + (((j * 2 + (kq >> 1)) ^ (l16 & 7)) << 4) +
+                                       (kq & 1) * 8) =
+          u32x2{to_bf16x2(acc[i][j][0], acc[i][j][1]), to_bf16x2(acc[i][j][2], acc[i][j][3])};
+    u32x4 o[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+      o[s] = *reinterpret_cast<const LDS_AS u32x4*>(buf + (s * 8 + m8) * 128 + ((c8 ^ m8) << 4));
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int ri = row0 + i * 16 + s * 8 + m8;
+      if (ri < t.i_valid) store_far(out + (size_t)(t.i0 + ri) * p.ldo + col, n, o[s]);
+    }
+  }
+}
+
+// GATHER: rows of x come through perm.
+template <bool GATHER>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void grouped_fp8_kernel(GroupedParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem_raw[kFp8Lds];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const int grp = wave >> 2, w4 = wave & 3;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem_raw);
+  const LDS_AS char* smem = (const LDS_AS char*)smem_raw;
+  const int nk = ceil_div(p.K, 128);
+  const int chunks = p.K / 16;
+
+  const int mt = ((const CONST_AS i32x4*)p.row_tiles)[0][0];
+  const int nt = ceil_div(p.N, kB);
+  const int total = mt * nt;
+  GroupedTile t;
+
+  // Loads: instruction q of wave w moves rows (w + 4q)*8 .. +8 of its group's operand
+  // (lane l: row l/8, chunk l%8, swapped as the fragment reads expect)
+  const int my_chunk = (lane & 7) ^ swz_along(w4 * 8 + (lane >> 3));
+  const char* base = nullptr;    // of the group's operand
+  uint32_t bytes = 0, off0 = 0;  // off0: of the first instruction's rows
+  uint32_t s_off = 0;            // group 0: of this lane's scale
+  const char* s_base = nullptr;
+  uint32_t s_bytes = 0;
+
+  auto locate = [&](int id) INLINE {
+    const GroupedParams p = fresh_params();
+    id = xcd_window_remap(id, total);
+    int tm, tn;
+    tile_of(id, mt, nt, tm, tn);
+    const i32x4 r = ((const CONST_AS i32x4*)p.row_tiles)[1 + uniform(tm)];
+    t.e = r[0];
+    t.beg = t.end = 0;
+    t.i0 = r[1];
+    t.i_valid = r[2];
+    t.j0 = uniform(tn) * kB;
+    if (grp == 0) {
+      base = GATHER ? p.a : p.a + (long long)t.i0 * p.K;
+      bytes = (uint32_t)((long long)(GATHER ? p.R / p.k : t.i_valid) * p.K);
+      const long long s_row = 4LL * nk;
+      s_base = reinterpret_cast<const char*>(p.row_scale) + (GATHER ? 0 : t.i0 * s_row);
+      s_bytes = (uint32_t)((GATHER ? p.R / p.k : t.i_valid) * s_row);
+      const int row = min(w4 * 64 + lane, t.i_valid - 1);
+      s_off = (uint32_t)((GATHER ? source_row(p, t.i0 + row) : row) * s_row);
+      if constexpr (GATHER) {
+        // the rows this wave loads, eight to an instruction (rows past the tile's repeat one
+        // that exists; their results are not stored)
+        const int mine = (w4 + 4 * (lane >> 3)) * 8 + (lane & 7);
+        *(LDS_AS uint32_t*)((LDS_AS char*)smem_raw + kOffsets + (w4 * 64 + lane) * 4) =
+            (uint32_t)(source_row(p, t.i0 + min(mine, t.i_valid - 1)) * p.K);
+      }
+    } else {
+      base = p.b + (size_t)t.e * p.N * p.K + (long long)t.j0 * p.K;
+      bytes = (uint32_t)((long long)min(kB, p.N - t.j0) * p.K);
+    }
+    off0 = (uint32_t)((w4 * 8 + (lane >> 3)) * p.K) + my_chunk * 16;
+  };
+  auto issue = [&](int kt) INLINE {
+    const uint32_t lds = opaque(lds0 + (grp * 2 + (kt & 1)) * kStage);
+    const uint32_t step = opaque((uint32_t)p.K * 32);
+    const i32x4 d = descriptor(base + (size_t)kt * 128, bytes - (uint32_t)kt * 128);
+    const bool in = kt * 8 + my_chunk < chunks;
+    if (GATHER && grp == 0) {
+      const LDS_AS char* at = smem + kOffsets + (w4 * 64 + (lane >> 3)) * 4;
+#pragma unroll
+      for (int q = 0; q < kInst; ++q)
+        load_lds16(d, in ? *reinterpret_cast<const LDS_AS uint32_t*>(at + q * 32) + my_chunk * 16
+                         : kNowhere, lds + (w4 + 4 * q) * 1024);
+    } else {
+#pragma unroll
+      for (int q = 0; q < kInst; ++q)
+        load_lds16(d, in ? off0 + q * step : kNowhere, lds + (w4 + 4 * q) * 1024);
+    }
+    if (grp == 0)
+      load_lds4(descriptor(s_base + (size_t)kt * 4, s_bytes - (uint32_t)kt * 4), s_off,
+                opaque(lds0 + kScales + (kt & 1) * 1024) + w4 * 256);
+  };
+
+  // fragments: lane l holds row or column l % 16 of a block and 32 bytes of the sum, the
+  // quarter l / 16 of the tile
+  const int l16 = lane & 15, kq = lane >> 4;
+  const int at16 = l16 * 128 + (((2 * kq) ^ swz_along(l16)) << 4);
+  f32x4 acc[8][4];
+  struct Frags {
+    i32x8 a[8], b[4];
+    float f[8];  // scale of the block's rows times the columns'
+  };
+  const CONST_AS float* col_scale = nullptr;
+  auto fragment = [&](const LDS_AS char* block, int at) INLINE {
+    // (swz_along is the same for rows 16 apart; the second chunk is the first's neighbour)
+    const u32x4 lo = *reinterpret_cast<const LDS_AS u32x4*>(block + at);
+    const u32x4 hi = *reinterpret_cast<const LDS_AS u32x4*>(block + (at ^ 16));
+    return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3],
+                 (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
+  };
+  auto load_frags = [&](auto mb, int kt, Frags& f) INLINE {
+    const LDS_AS char* sa = smem + (kt & 1) * kStage + grp * 128 * 128;
+    const LDS_AS char* sb = smem + (2 + (kt & 1)) * kStage + w4 * 64 * 128;
+    const LDS_AS char* sc = smem + kScales + (kt & 1) * 1024 + (grp * 128 + l16) * 4;
+    int at = at16;
+    asm volatile("" : "+v"(at));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f.b[j] = fragment(sb + j * 2048, at);
+    const float col = col_scale[kt];
+#pragma unroll
+    for (int i = 0; i < decltype(mb)::value; ++i) {
+      f.a[i] = fragment(sa + i * 2048, at);
+      f.f[i] = *reinterpret_cast<const LDS_AS float*>(sc + i * 64) * col;
+    }
+    // the stages may be filled again behind the next barriers
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+  // One instruction for each 16 x 16 block, whose sums are added three blocks later: by then
+  // they are there (one behind costs 90% more time than the instructions alone, two 30%,
+  // three 14%).
+  auto mfmas = [&](auto mb, const Frags& f) INLINE {
+    constexpr int BLOCKS = decltype(mb)::value * 4, BEHIND = 3;
+    __builtin_amdgcn_s_setprio(1);
+    f32x4 part[BEHIND + 1];
+#pragma unroll
+    for (int n = 0; n < BLOCKS + BEHIND; ++n) {
+      if (n < BLOCKS)
+        part[n % (BEHIND + 1)] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+            f.b[n % 4], f.a[n / 4], f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
+      if (n >= BEHIND) {
+        const int m = n - BEHIND;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          acc[m / 4][m % 4][v] = fmaf(part[m % (BEHIND + 1)][v], f.f[m / 4], acc[m / 4][m % 4][v]);
+        // (here and now: the compiler moves sums that the next tile needs first to where that
+        // starts, behind the barrier, and holds all 32 blocks until then)
+        asm volatile("" : "+v"(acc[m / 4][m % 4]));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    __builtin_amdgcn_s_setprio(0);
+  };
+  auto phase_end = [&]() INLINE {
+    __builtin_amdgcn_sched_barrier(0);
+    lds_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto start = [&]() INLINE {
+    issue(0);
+    if (nk > 1) issue(1);
+  };
+  auto walk = [&](auto mb) INLINE {
+    constexpr bool LIVE = decltype(mb)::value > 0;
+    if (grp == 0) {
+#pragma unroll 1
+      for (int kt = 0; kt < nk; ++kt) {
+        if (kt >= 1 && kt + 1 < nk) issue(kt + 1);
+        Frags f;
+        if constexpr (LIVE) load_frags(mb, kt, f);
+        phase_end();
+        if constexpr (LIVE) mfmas(mb, f);
+        if (kt >= 1) wait_vmcnt<0>();
+        phase_end();
+      }
+    } else {
+      phase_end();
+#pragma unroll 1
+      for (int kt = 0; kt < nk; ++kt) {
+        Frags f;
+        if constexpr (LIVE) load_frags(mb, kt, f);
+        wait_vmcnt<0>();
+        phase_end();
+        if (kt + 2 < nk) issue(kt + 2);
+        if constexpr (LIVE) mfmas(mb, f);
+        if (kt + 1 < nk) phase_end();
+      }
+    }
+  };
+
+  int id = blockIdx.x;
+  if (id >= total) return;
+  locate(id);
+  start();
+  wait_vmcnt<0>();
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    phase_end();
+    const int rows = t.j0 + w4 * 64 < p.N ? t.i_valid - grp * 128 : 0;
+    if (rows > 0)
+      col_scale = (const CONST_AS float*)(p.col_scale + ((size_t)t.e * ceil_div(p.N, 128) +
+                                                         (t.j0 + w4 * 64) / 128) * nk);
+    if (rows > 64) walk(std::integral_constant<int, 8>{});
+    else if (rows > 0) walk(std::integral_constant<int, 4>{});
+    else walk(std::integral_constant<int, 0>{});
+    // the next results' first tiles go ahead of the stores (the last barrier is behind every
+    // wave's fragment reads) and have landed when the stores start
+    const GroupedTile done = t;
+    id += gridDim.x;
+    const bool more = id < total;
+    if (more) {
+      locate(id);
+      start();
+    }
+    store_fp8_results(fresh_params(), done, grp * 128, done.j0 + w4 * 64, acc,
+                      (LDS_AS char*)smem_raw + kOut + wave * 2048, [&]() { wait_vmcnt<0>(); });
+    if (!more) break;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_grouped_fp8_pp(const GroupedParams& p, long long tiles, hipStream_t stream) {
+  if (tiles > 0x7fffffffLL || p.splits != 1 || p.out_fp32) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(row_tiles_kernel, dim3(1), dim3(1024), 0, stream, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // one workgroup to a CU
+  const dim3 grid((unsigned)std::min<long long>(tiles, 256)), block(kThreads);
+  if (p.perm)
+    hipLaunchKernelGGL(grouped_fp8_kernel<true>, grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL(grouped_fp8_kernel<false>, grid, block, 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace eaas

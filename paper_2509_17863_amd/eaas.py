@@ -530,11 +530,11 @@ _GROUPED_KERNELS = ("any", "few", "large")
 
 def _grouped_plan(product: str, R, E, N, K, in16: bool) -> tuple[str, int, int]:
     """(kernel, rows of its tiles, parts of the sum) of the product "forward", "dx",
-    "dw", "int8", "fp8", "swiglu" or "swiglu_backward": the library's own choice, asked
-    on the host, for tests and measurements.  in16: sizes, strides and bases are
-    multiples of 16 bytes."""
+    "dw", "int8", "fp8" (bf16 results), "fp8_fp32", "swiglu" or "swiglu_backward": the
+    library's own choice, asked on the host, for tests and measurements.  in16: sizes,
+    strides and bases are multiples of 16 bytes."""
     s = _group_shape(R, E, N, K)
-    d, kind = {"forward": (0, 0), "dx": (1, 0), "dw": (2, 0), "int8": (0, 1), "fp8": (0, 2),
+    d, kind = {"forward": (0, 0), "dx": (1, 0), "dw": (2, 0), "int8": (0, 1), "fp8": (0, 2), "fp8_fp32": (0, 4),
                "swiglu": (0, 3), "swiglu_backward": (1, 3)}[product]
     r = int(lib().eaas_internal_grouped_plan(ctypes.byref(s), d, kind, int(in16)))
     if r < 0:

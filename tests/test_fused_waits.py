@@ -1,4 +1,4 @@
-"""Waits of the large-tile kernels with an epilogue, followed as in test_grouped_waits.py:
+"""Waits of the large-tile kernels with an epilogue and of e4m3, followed as in test_grouped_waits.py:
 no wave passes a bare barrier with an LDS access of its own under way."""
 import re
 import subprocess
@@ -8,7 +8,8 @@ from test_grouped_waits import under_way_at_barriers
 
 from paper_2509_17863_amd import _build
 
-SOURCES = {"grouped_swiglu.hip": ("grouped_pp_kernel", 3)}  # gathered or not, and the way back
+SOURCES = {"grouped_swiglu.hip": ("grouped_pp_kernel", 3),  # gathered or not, and the way back
+           "grouped_fp8.hip": ("grouped_fp8_kernel", 2)}    # gathered or not
 
 
 def kernels(source, out):

@@ -204,9 +204,9 @@ class Case:
         self.scratch = eaas.alloc_grouped_fp8_workspace(R, E, N, K)
         self.scratch.fill_(0xFF)
 
-    def plan(self, in16=None):
-        return eaas._grouped_plan("fp8", self.R, self.E, self.N, self.K,
-                                  self.K % 16 == 0 if in16 is None else in16)
+    def plan(self, dtype, in16=None):
+        return eaas._grouped_plan("fp8" if dtype == torch.bfloat16 else "fp8_fp32", self.R, self.E,
+                                  self.N, self.K, self.K % 16 == 0 if in16 is None else in16)
 
     def run(self, dtype, pad=0, **kw):
         wide = torch.full((self.R, self.N + pad), CANARY, dtype=dtype, device="cuda")
@@ -221,7 +221,7 @@ class Case:
 
     def check(self, y, in16=None):
         want, mag = self.want()
-        kernel, _, parts = self.plan(in16)
+        kernel, _, parts = self.plan(y.dtype, in16)
         rel = (128 + blocks(self.K) + parts * 4 + 2) * 2.0 ** -23
         if kernel == "large" and y.dtype == torch.bfloat16:
             rel += 7 * 2.0 ** -14
@@ -271,10 +271,22 @@ def test_codes_from_any_byte(gpu, shape, dtype):
     c.check(c.run(dtype, pad=shape[-2]), in16=False)
 
 
-EXACT = [(1, 1, 40, 9000, "one", 0), (20, 2, 96, 4096, "some", 4), (64, 1, 64, 8192, "even", 0),
+EXACT = [(5, 1, 40, 70000, "one", 0), (20, 2, 96, 4096, "some", 4), (64, 1, 64, 8192, "even", 0),
          (200, 2, 264, 9008, "one", 4), (9, 2, 33, 30001, "even", 3), (512, 16, 1024, 2048, "ragged", 2),
          (3000, 5, 6200, 528, "ragged", 0), (3000, 4, 6201, 1040, "some", 4),
          (2600, 5, 6144, 1300, "ragged", 0)]
+
+
+def test_every_kernel_is_among_these():
+    """On the host: every way of computing the product, in one part and in several."""
+    seen = set()
+    for R, E, N, K, *_ in EXACT:
+        for product in ("fp8", "fp8_fp32"):
+            kernel, rows, parts = eaas._grouped_plan(product, R, E, N, K, K % 16 == 0)
+            seen.add((product, kernel, rows if kernel == "few" else 0, parts > 1))
+    for want in [("fp8", "large", 0, False), ("fp8", "any", 0, False), ("fp8", "any", 0, True),
+                 ("fp8", "few", 16, True), ("fp8", "few", 64, True), ("fp8", "few", 64, False)]:
+        assert want in seen, (want, seen)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
