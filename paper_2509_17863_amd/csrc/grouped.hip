@@ -142,27 +142,44 @@ __device__ __forceinline__ u32x4 fragment(const LDS_AS char* stage, int c0, int 
   }
 }
 
-// The sum over a block of 128 e4m3 elements for 32 rows from a0 and 32 columns from b0:
+// The sums over a block of 128 e4m3 elements for 64 rows from a0 and 64 columns from b0:
 // codes go to bf16, which holds them exactly, products of those are exact in fp32 and are
 // summed there.  (The 8-bit floating matrix instructions keep less: see grouped_fp8.hip.)
 // A lane's 16 codes make two steps of the sum, whose order both operands share.
-__device__ __forceinline__ f32x16 fp8_block(const LDS_AS char* sa, int a0, const LDS_AS char* sb,
-                                            int b0) {
-  f32x16 part = {};
+__device__ __forceinline__ void fp8_block(const LDS_AS char* sa, int a0, const LDS_AS char* sb,
+                                          int b0, f32x16 (&part)[2][2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) part[i][j] = f32x16{};
 #pragma unroll
   for (int kk = 0; kk < 4; ++kk) {
-    const u32x4 a = fragment<false>(sa, a0, kk), b = fragment<false>(sb, b0, kk);
+    u32x4 a[2], b[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      part = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          fp8x8_to_bf16(u32x2{b[2 * h], b[2 * h + 1]}), fp8x8_to_bf16(u32x2{a[2 * h], a[2 * h + 1]}),
-          part, 0, 0, 0);
+    for (int i = 0; i < 2; ++i) {
+      a[i] = fragment<false>(sa, a0 + 32 * i, kk);
+      b[i] = fragment<false>(sb, b0 + 32 * i, kk);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 fa[2], fb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fa[i] = fp8x8_to_bf16(u32x2{a[i][2 * h], a[i][2 * h + 1]});
+        fb[i] = fp8x8_to_bf16(u32x2{b[i][2 * h], b[i][2 * h + 1]});
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          part[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], part[i][j], 0, 0, 0);
+    }
   }
-  return part;
 }
 
 template <int DIR, int TYPE, int EPI>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3)))
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(TYPE == kFp8 ? 2 : 3, TYPE == kFp8 ? 2 : 3)))
 void grouped_any_kernel(GroupedParams p) {
   constexpr bool A_ACROSS = DIR == kGradWeights, B_ACROSS = DIR != kForward;
   constexpr bool I8 = TYPE == kInt8, FP8 = TYPE == kFp8;
@@ -251,18 +268,15 @@ void grouped_any_kernel(GroupedParams p) {
       if (kt + 1 < last) load(kt + 1);
       const LDS_AS char *sa = lds, *sb = lds + kStage;
       if constexpr (FP8) {
+f32x16 part[2][2];
+        fp8_block(sa, wi, sb, wj, part);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const float f = row_scale[i][kt] * col_scale[kt];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const f32x16 part = fp8_block(sa, wi + 32 * i, sb, wj + 32 * j);
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = fmaf(part[v], f, acc[i][j][v]);
-            // (one block at a time: with the fragments of all four read ahead, 300
-            // registers went to memory)
-            __builtin_amdgcn_sched_barrier(0);
-          }
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = fmaf(part[i][j][v], f, acc[i][j][v]);
         }
         __syncthreads();
         continue;
