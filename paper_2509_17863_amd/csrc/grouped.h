@@ -290,6 +290,9 @@ hipError_t launch_grouped_swiglu_grad_pp(const GroupedParams& p, long long tiles
 // grouped_fp8.hip: the same for block-scaled e4m3, bf16 results.
 hipError_t launch_grouped_fp8_pp(const GroupedParams& p, long long tiles, hipStream_t stream);
 
+// The same operands on 128 x 128 tiles, fp32 sums of exact products.
+hipError_t launch_grouped_fp8_mid(const GroupedParams& p, long long tiles, hipStream_t stream);
+
 // grouped_few.hip: tiles of `rows` (16, 32 or 64) x 64 under the same condition.
 template <int DIR, int TYPE, int EPI>
 hipError_t launch_grouped_few(const GroupedParams& p, int rows, long long tiles,

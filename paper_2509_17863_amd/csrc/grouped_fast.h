@@ -1,5 +1,5 @@
 // Parts shared by the grouped product kernels: loads straight into LDS, the order
-// of chunks there, and the way out of the results.
+// of chunks there, fragments, and the way out of the results.
 #pragma once
 
 #include <type_traits>
@@ -43,6 +43,68 @@ __device__ __forceinline__ int swz_along(int row) { return (row & 7) ^ ((row >> 
 // bytes: the four rows' chunks go to distinct banks in both views (32 banks or 64).
 __device__ __forceinline__ int swz_across(int row) {
   return ((row & 1) << 2) | (((row >> 1) & 1) * 10);
+}
+
+// Fragment of k-step kk for the 32 rows (along) or columns (across) from c0: lane
+// l holds element l % 32 and 16 bytes of the sum, the half l / 32 of the step.
+template <bool ACROSS>
+__device__ __forceinline__ u32x4 fragment(const LDS_AS char* stage, int c0, int kk) {
+  const int lane = threadIdx.x & (kWave - 1);
+  if constexpr (ACROSS) {
+    const int g = lane >> 4, i = lane & 15;
+    const int c = c0 + (g & 1) * 16 + (i & 3) * 4;
+    u32x4 f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int s = kk * 16 + (g >> 1) * 8 + h * 4 + (i >> 2);
+      const LDS_AS char* at = stage + s * 256 + (((c >> 3) ^ swz_across(s)) << 4) + (c & 7) * 2;
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      const s16x4 t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_AS s16x4*)at);
+      const u32x2 w = __builtin_bit_cast(u32x2, t);
+      f[2 * h] = w[0];
+      f[2 * h + 1] = w[1];
+    }
+    return f;
+  } else {
+    const int r = c0 + (lane & 31);
+    return *reinterpret_cast<const LDS_AS u32x4*>(stage + r * 128 +
+                                                  (((2 * kk + (lane >> 5)) ^ swz_along(r)) << 4));
+  }
+}
+
+// The sums over a block of 128 e4m3 elements for 64 rows from a0 and 64 columns from b0:
+// codes go to bf16, which holds them exactly, products of those are exact in fp32 and are
+// summed there.  (The 8-bit floating matrix instructions keep less: see grouped_fp8.hip.)
+// A lane's 16 codes make two steps of the sum, whose order both operands share.
+__device__ __forceinline__ void fp8_block(const LDS_AS char* sa, int a0, const LDS_AS char* sb,
+                                          int b0, f32x16 (&part)[2][2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) part[i][j] = f32x16{};
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk) {
+    u32x4 a[2], b[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      a[i] = fragment<false>(sa, a0 + 32 * i, kk);
+      b[i] = fragment<false>(sb, b0 + 32 * i, kk);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 fa[2], fb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fa[i] = fp8x8_to_bf16(u32x2{a[i][2 * h], a[i][2 * h + 1]});
+        fb[i] = fp8x8_to_bf16(u32x2{b[i][2 * h], b[i][2 * h + 1]});
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          part[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[j], fa[i], part[i][j], 0, 0, 0);
+    }
+  }
 }
 
 // A wave's results, MBW x 2 blocks of 32 x 32, to memory: rows row0.. of the tile,

@@ -272,7 +272,106 @@ void grouped_fp8_kernel(GroupedParams p) {
   }
 }
 
+// The product on 128 x 128 tiles with codes converted to bf16 as fragments are read.  Four
+// waves, 64 x 64 results each, two LDS stages of both operands: a tile's loads are started
+// when every wave has read what the stage held, and waited for a tile later.  Two
+// workgroups to a CU cover each other's barriers, starts and stores.
+constexpr int kMidThreads = 256, kMidOperand = 16384, kMidStage = 2 * kMidOperand + 512;
+
+__global__ __launch_bounds__(kMidThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void grouped_fp8_mid_kernel(GroupedParams p) {
+  __shared__ __attribute__((aligned(1024))) char smem_raw[2 * kMidStage];
+  static_assert(4 * kWayOutBytes <= 2 * kMidStage, "way out");
+  GroupedTile t;
+  if (!find_tile<kForward, 128, 128, kMidThreads>(p, reinterpret_cast<int*>(smem_raw), t)) return;
+
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem_raw);
+  const LDS_AS char* smem = (const LDS_AS char*)smem_raw;
+  const int kb = ceil_div(p.K, 128), chunks = p.K / 16;
+  const int first = (int)((long long)kb * blockIdx.y / p.splits);
+  const int last = (int)((long long)kb * (blockIdx.y + 1) / p.splits);
+
+  // loads: instruction q of wave w moves rows (w + 4q)*8 .. +8 of both operands
+  const int row0 = wave * 8 + (lane >> 3);
+  const int my_chunk = (lane & 7) ^ swz_along(row0);
+  const bool gather = p.perm != nullptr;
+  const long long rows = gather ? p.R / p.k : t.i_valid;
+  const char* a_base = p.a + (gather ? 0 : (long long)t.i0 * p.K);
+  const char* b_base = p.b + ((size_t)t.e * p.N + t.j0) * p.K;
+  const char* s_base = reinterpret_cast<const char*>(p.row_scale + (gather ? 0 : (size_t)t.i0 * kb));
+  const uint32_t a_bytes = (uint32_t)(rows * p.K), s_bytes = (uint32_t)(rows * kb * 4);
+  const uint32_t b_bytes = (uint32_t)((long long)min(128, p.N - t.j0) * p.K);
+  auto source = [&](int row) {
+    row = min(row, t.i_valid - 1);
+    return gather ? source_row(p, t.i0 + row) : row;
+  };
+  uint32_t a_off[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) a_off[q] = (uint32_t)(source(row0 + 32 * q) * p.K) + my_chunk * 16;
+  const uint32_t b_off = (uint32_t)(row0 * p.K) + my_chunk * 16, step = (uint32_t)p.K * 32;
+  const uint32_t s_off = (uint32_t)(source((wave & 1) * 64 + lane) * 4LL * kb);
+  auto issue = [&](int kt) {
+    const uint32_t dst = lds0 + (kt & 1) * kMidStage + wave * 1024;
+    const bool in = kt * 8 + my_chunk < chunks;
+    const i32x4 da = descriptor(a_base + (size_t)kt * 128, a_bytes - (uint32_t)kt * 128);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) load_lds16(da, in ? a_off[q] : kNowhere, dst + q * 4096);
+    const i32x4 db = descriptor(b_base + (size_t)kt * 128, b_bytes - (uint32_t)kt * 128);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      load_lds16(db, in ? b_off + q * step : kNowhere, dst + kMidOperand + q * 4096);
+    if (wave < 2)
+      load_lds4(descriptor(s_base + (size_t)kt * 4, s_bytes - (uint32_t)kt * 4), s_off,
+                lds0 + (kt & 1) * kMidStage + 2 * kMidOperand + wave * 256);
+  };
+
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) acc[i][j] = f32x16{};
+  const int wi = (wave & 1) * 64, wj = (wave >> 1) * 64;
+  const CONST_AS float* col_scale =
+      (const CONST_AS float*)(p.col_scale + ((size_t)t.e * ceil_div(p.N, 128) + t.j0 / 128) * kb);
+  if (first < last) issue(first);
+#pragma unroll 1
+  for (int kt = first; kt < last; ++kt) {
+    // this tile has landed, and every wave has read the one before
+    wait_vmcnt<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    lds_barrier();
+    if (kt + 1 < last) issue(kt + 1);
+    const LDS_AS char* stage = smem + (kt & 1) * kMidStage;
+    const float col = col_scale[kt];
+    f32x16 part[2][2];
+    fp8_block(stage, wi, stage + kMidOperand, wj, part);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float f = *reinterpret_cast<const LDS_AS float*>(stage + 2 * kMidOperand +
+                                                             (wi + 32 * i + (lane & 31)) * 4) * col;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][j][v] = fmaf(part[i][j][v], f, acc[i][j][v]);
+        asm volatile("" : "+v"(acc[i][j]));  // (not behind the next barrier)
+      }
+    }
+  }
+  __syncthreads();
+  way_out<kForward, kBf16>(p, t, blockIdx.y, wi, t.j0 + wj, acc,
+                           (LDS_AS float*)(smem_raw + wave * kWayOutBytes));
+}
+
 }  // namespace
+
+hipError_t launch_grouped_fp8_mid(const GroupedParams& p, long long tiles, hipStream_t stream) {
+  if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(grouped_fp8_mid_kernel, tile_grid(tiles, p.splits), dim3(kMidThreads), 0,
+                     stream, p);
+  return hipGetLastError();
+}
 
 hipError_t launch_grouped_fp8_pp(const GroupedParams& p, long long tiles, hipStream_t stream) {
   if (tiles > 0x7fffffffLL || p.splits != 1 || p.out_fp32) return hipErrorInvalidValue;

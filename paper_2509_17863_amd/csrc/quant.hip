@@ -97,6 +97,12 @@ __device__ __forceinline__ void load_values(const void* x, long long at, int n, 
   }
 }
 
+// The row of unit u, kb units to a row.  (A 64-bit quotient costs as much as the rest of a
+// unit.)
+__device__ __forceinline__ long long row_of(long long u, int kb) {
+  return u >> 32 ? u / kb : (long long)((uint32_t)u / (uint32_t)kb);
+}
+
 // Rows of any length, stride and alignment, a scale for each 128 columns: 16 lanes
 // take a block.
 template <bool FP32>
@@ -108,7 +114,7 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_row_blocks_kernel(
   const int l = threadIdx.x & 15;
   for (long long u = ((long long)blockIdx.x * kQuantThreads + threadIdx.x) >> 4; u < total;
        u += (long long)gridDim.x * (kQuantThreads / 16)) {
-    const long long r = u / kb;
+    const long long r = row_of(u, kb);
     const int b = (int)(u - r * kb), c = b * 128 + l * 8, n = K - c;
     float v[8];
     load_values<FP32>(x, r * ldx + c, n, v);
@@ -158,6 +164,15 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_blocks_kernel(
   }
 }
 
+// Finite values to e4m3 codes.
+__device__ __forceinline__ float within_448(float v) {
+  return __builtin_amdgcn_fmed3f(v, -448.0f, 448.0f);
+}
+__device__ __forceinline__ uint32_t pack_codes(float a, float b, float c, float d) {
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
 // silu(gate) * up in 64 bits, rounded once to fp32.
 __device__ __noinline__ float silu_up_64(float g, float up) {
   return (float)((double)g / (1.0 + exp(-(double)g)) * (double)up);
@@ -180,7 +195,7 @@ __global__ __launch_bounds__(kQuantThreads) void swiglu_fp8_kernel(
   const int l = threadIdx.x & 15;
   for (long long u = ((long long)blockIdx.x * kQuantThreads + threadIdx.x) >> 4; u < total;
        u += (long long)gridDim.x * (kQuantThreads / 16)) {
-    const long long r = u / kb;
+    const long long r = row_of(u, kb);
     const int b = (int)(u - r * kb), c = b * 128 + l * 8, n = I - c;
     const uint16_t* row = gu + r * 2 * I + c;
     float g[8], up[8], v[8];
@@ -188,16 +203,27 @@ __global__ __launch_bounds__(kQuantThreads) void swiglu_fp8_kernel(
     load8(row + I, n, up);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = silu_full_up(g[i], up[i]);
-    const uint32_t m = largest16(largest8(v, 0));
+    const uint32_t mine = largest8(v, 0), m = largest16(mine);
     const bool ends = m - 0x0d000000u >= 0x70000000u;  // below 2^-101 or from 2^123 on
-    // the values that may be the block's largest, in 64 bits
+    // the values that may be the block's largest, in 64 bits: one, as a rule
     uint32_t most = 0;
     const uint32_t near = ends ? 0 : m - 16;
-#pragma unroll 1
-    for (int i = 0; i < 8; ++i) {
-      const float a = v[i];
-      if (m != 0 && (__float_as_uint(a) & 0x7fffffffu) >= near)
-        most = max(most, __float_as_uint(silu_up_64(g[i], up[i])) & 0x7fffffffu);
+    if (m != 0 && mine >= near) {
+      uint32_t left = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        left |= (__float_as_uint(v[i]) & 0x7fffffffu) >= near ? 1u << i : 0u;
+      do {
+        const int at = __builtin_ctz(left);
+        float ga = g[0], ua = up[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) {
+          ga = at == i ? g[i] : ga;
+          ua = at == i ? up[i] : ua;
+        }
+        most = max(most, __float_as_uint(silu_up_64(ga, ua)) & 0x7fffffffu);
+        left &= left - 1;
+      } while (left);
     }
     most = largest16(most);
     const float sc = block_scale(most);
@@ -208,8 +234,11 @@ __global__ __launch_bounds__(kQuantThreads) void swiglu_fp8_kernel(
       uint32_t w2[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        w[h] = pack_e4m3x4(v[4 * h] * lo, v[4 * h + 1] * lo, v[4 * h + 2] * lo, v[4 * h + 3] * lo);
-        w2[h] = pack_e4m3x4(v[4 * h] * hi, v[4 * h + 1] * hi, v[4 * h + 2] * hi, v[4 * h + 3] * hi);
+        // (the smaller quotients are at most 448 by themselves)
+        const float* x = v + 4 * h;
+        w[h] = pack_codes(x[0] * lo, x[1] * lo, x[2] * lo, x[3] * lo);
+        w2[h] = pack_codes(within_448(x[0] * hi), within_448(x[1] * hi), within_448(x[2] * hi),
+                           within_448(x[3] * hi));
       }
       if (ends || w[0] != w2[0] || w[1] != w2[1]) {
 #pragma unroll 1
@@ -231,7 +260,7 @@ __global__ __launch_bounds__(kQuantThreads) void swiglu_fp8_kernel(
 // Workgroups of a pass over `units` of 16 lanes each.
 unsigned unit_grid(long long units) {
   return (unsigned)std::min<long long>((units + kQuantThreads / 16 - 1) / (kQuantThreads / 16),
-                                       1 << 16);
+                                       8192);
 }
 
 }  // namespace

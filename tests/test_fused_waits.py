@@ -8,8 +8,9 @@ from test_grouped_waits import under_way_at_barriers
 
 from paper_2509_17863_amd import _build
 
-SOURCES = {"grouped_swiglu.hip": ("grouped_pp_kernel", 3),  # gathered or not, and the way back
-           "grouped_fp8.hip": ("grouped_fp8_kernel", 2)}    # gathered or not
+# (source, kernel, how many of it): gathered or not, and the way back; gathered or not
+KERNELS = [("grouped_swiglu.hip", "grouped_pp_kernel", 3), ("grouped_fp8.hip", "grouped_fp8_kernel", 2),
+           ("grouped_fp8.hip", "grouped_fp8_mid_kernel", 1)]
 
 
 def kernels(source, out):
@@ -30,9 +31,8 @@ def kernels(source, out):
     return found
 
 
-@pytest.mark.parametrize("source", SOURCES)
-def test_no_lds_access_is_under_way_at_a_barrier(source, tmp_path):
-    kernel, count = SOURCES[source]
+@pytest.mark.parametrize("source,kernel,count", KERNELS)
+def test_no_lds_access_is_under_way_at_a_barrier(source, kernel, count, tmp_path):
     large = {n: k for n, k in kernels(source, tmp_path / "a.s").items() if kernel in n}
     assert len(large) == count
     for name, lines in large.items():
