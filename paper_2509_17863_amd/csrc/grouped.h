@@ -257,25 +257,82 @@ __device__ __forceinline__ void store_swiglu(const GroupedParams& p, size_t i, i
   }
 }
 
-// kSwigluGrad, from dh.  (The result may lie over gate and up: they are read before.)
-__device__ __forceinline__ void store_swiglu_grad(const GroupedParams& p, size_t i, int j, int n,
-                                                  const float (&dh)[8]) {
-  const uint16_t* from = p.gu + i * p.ldgu + j;
-  float g[8], u[8];
-  load8(from, n, g);
-  load8(from + p.K, n, u);
-  float dg[8], du[8], h[8];
+// kSwigluGrad: gate and up of eight columns as they come, and what dh makes of them.  (The
+// result may lie over gate and up, so the compiler keeps their loads behind earlier stores:
+// where several are to be in flight, they are all taken first.)
+struct GateUp {
+  u32x4 gate, up;
+};
+__device__ __forceinline__ u32x4 load8_raw(const uint16_t* p, int n) {
+  u32x4 v = {0, 0, 0, 0};
+  if (n >= 8) {
+    __builtin_memcpy(&v, p, 16);
+  } else if (n > 0) {
+    // (every element is loaded, the last one repeatedly: loads under a condition each would
+    // be waited for one by one)
+    uint32_t e[8];
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    const SwigluGrad t = swiglu_grad(g[c], u[c], dh[c]);
-    dg[c] = t.gate;
-    du[c] = t.up;
-    h[c] = silu_up(g[c], u[c]);
+    for (int c = 0; c < 8; ++c) e[c] = p[min(c, n - 1)];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c / 2] |= (c < n ? e[c] : 0u) << (16 * (c & 1));
+  }
+  return v;
+}
+__device__ __forceinline__ GateUp load_gate_up(const GroupedParams& p, size_t i, int j, int n) {
+  const uint16_t* from = p.gu + i * p.ldgu + j;
+  return {load8_raw(from, n), load8_raw(from + p.K, n)};
+}
+// (far: past the caches, for results of large products)
+typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+__device__ __forceinline__ void store8_raw(uint16_t* at, int n, u32x4 v, bool far) {
+  if (n >= 8) {
+    if (far) __builtin_nontemporal_store(v, reinterpret_cast<any4*>(at));
+    else __builtin_memcpy(at, &v, 16);
+  } else {
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      if (c < n) at[c] = (uint16_t)(v[c / 2] >> (16 * (c & 1)));
+  }
+}
+__device__ __forceinline__ void store_swiglu_grad(const GroupedParams& p, size_t i, int j, int n,
+                                                  const GateUp& x, const float (&dh)[8], bool far) {
+  u32x4 dg, du, h;
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const float g0 = __uint_as_float(x.gate[c] << 16), u0 = __uint_as_float(x.up[c] << 16);
+    const float g1 = __uint_as_float(x.gate[c] & 0xffff0000u);
+    const float u1 = __uint_as_float(x.up[c] & 0xffff0000u);
+    const SwigluGrad t0 = swiglu_grad(g0, u0, dh[2 * c]), t1 = swiglu_grad(g1, u1, dh[2 * c + 1]);
+    dg[c] = to_bf16x2(t0.gate, t1.gate);
+    du[c] = to_bf16x2(t0.up, t1.up);
+    h[c] = to_bf16x2(silu_up(g0, u0), silu_up(g1, u1));
   }
   uint16_t* to = static_cast<uint16_t*>(p.out) + i * p.ldo + j;
-  store8(to, n, dg);
-  store8(to + p.K, n, du);
-  if (p.h) store8(p.h + i * p.ldh + j, n, h);
+  store8_raw(to, n, dg, far);
+  store8_raw(to + p.K, n, du, far);
+  if (p.h) store8_raw(p.h + i * p.ldh + j, n, h, far);
+}
+
+// Column j of row i alone: from the sums of gate and up, or dh.
+template <int EPI>
+__device__ __forceinline__ void store_one(const GroupedParams& p, size_t i, int j, float a, float b) {
+  uint16_t* to = static_cast<uint16_t*>(p.out) + i * p.ldo + j;
+  auto bits = [](float v) { return (uint16_t)to_bf16x2(v, 0.0f); };
+  if constexpr (EPI == kSwiglu) {
+    *to = bits(silu_up(a, b));
+    if (p.gu) {
+      p.gu[i * p.ldgu + j] = bits(a);
+      p.gu[i * p.ldgu + j + p.N / 2] = bits(b);
+    }
+  } else {
+    const uint16_t* from = p.gu + i * p.ldgu + j;
+    const float g = __uint_as_float((uint32_t)from[0] << 16);
+    const float u = __uint_as_float((uint32_t)from[p.K] << 16);
+    const SwigluGrad t = swiglu_grad(g, u, a);
+    to[0] = bits(t.gate);
+    to[p.K] = bits(t.up);
+    if (p.h) p.h[i * p.ldh + j] = bits(silu_up(g, u));
+  }
 }
 
 // grouped_fast.hip: 256 x 256 tiles, sizes and addresses in multiples of 16 bytes.

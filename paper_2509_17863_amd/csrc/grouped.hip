@@ -53,11 +53,29 @@ __device__ __forceinline__ u32x4 load_some(const char* p, int n) {
   return v;
 }
 
+// 16 bytes without the first n (1 to 15), zeros after the others.
+__device__ __forceinline__ u32x4 shift_down(u32x4 v, int n) {
+  uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
+  if (n >= 8) {
+    lo = hi;
+    hi = 0;
+  }
+  const int bits = (n & 7) * 8;
+  if (bits) {
+    lo = lo >> bits | hi << (64 - bits);
+    hi >>= bits;
+  }
+  return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+
 // One operand's tile on its way from memory to LDS.
 //   ACROSS: rows are the sum's index [s0, s0 + 64) up to s_end, columns
 //           [c0, c0 + 128) of `width`
 //   else:   128 rows (pointers fixed for the whole sum), 128 bytes of the sum
-template <bool ACROSS, int ESZ>
+//   TOGETHER: how tiles along an edge are loaded (dW, whose operands both lie across and
+//   whose sums are often shorter than a tile, keeps loads that nothing needs out: 4 rows
+//   an expert 157 us against 170; 8-bit integers have no registers left for the shift)
+template <bool ACROSS, int ESZ, bool TOGETHER>
 struct Loader {
   static constexpr int EPC = 16 / ESZ;  // elements of a chunk
   const char* row[4];                   // along: this thread's rows
@@ -92,12 +110,40 @@ struct Loader {
 #pragma unroll
       for (int q = 0; q < 4; ++q) v[q] = load16(at(q));
     } else {
+      // elements of chunk q that exist
+      auto left = [&](int q) {
+        return ACROSS ? (s_first + 16 * q < s_end ? width - c : 0) : s_end - s_first;
+      };
+      // (the shortest row that a whole chunk can be read from)
+      const int least = ACROSS ? width : s_end;
+      if (!TOGETHER || least < EPC) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          v[q] = u32x4{0, 0, 0, 0};
+          const int n = left(q);
+          if (n >= EPC) v[q] = load16(at(q));
+          else if (n > 0) v[q] = load_some<ESZ>(at(q), n);
+        }
+        return;
+      }
+      // A tile's loads go out together here too.  Every lane loads whole chunks: where its
+      // chunk ends inside, the last whole one of the row, which is then shifted down; where a
+      // row does not exist, one of a row that does.  (A branch around each load, and elements
+      // one by one, made the tiles along an edge take several times as long as the others:
+      // 1500 rows, 1003 x 1411, way back 69 us against 43.)
+      const int n = ACROSS ? width - c : s_end - s_first;
+      const int back = n > 0 && n < EPC ? (EPC - n) * ESZ : 0;
+      auto spare = [&](int q) {
+        return ACROSS ? rp(q, min(s_first + 16 * q, s_end - 1)) : row[ACROSS ? 0 : q];
+      };
+      if (n > 0) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = load16(left(q) > 0 ? at(q) - back : spare(q));
+      }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        v[q] = u32x4{0, 0, 0, 0};
-        const int n = ACROSS ? (s_first + 16 * q < s_end ? width - c : 0) : s_end - s_first;
-        if (n >= EPC) v[q] = load16(at(q));
-        else if (n > 0) v[q] = load_some<ESZ>(at(q), n);
+        if (left(q) <= 0) v[q] = u32x4{0, 0, 0, 0};
+        if (back) v[q] = shift_down(v[q], back);
       }
     }
   }
@@ -164,8 +210,9 @@ void grouped_any_kernel(GroupedParams p) {
         src[q] = source_row(p, min(t.beg + kt * SUM + (int)threadIdx.x / 16 + 16 * q, t.end - 1));
     }
   };
-  Loader<A_ACROSS, ESZ> la;
-  Loader<B_ACROSS, ESZ> lb;
+  constexpr bool TOGETHER = DIR != kGradWeights && !I8;
+  Loader<A_ACROSS, ESZ, TOGETHER> la;
+  Loader<B_ACROSS, ESZ, TOGETHER> lb;
   la.init(a_row);
   lb.init(b_row);
   auto load = [&](int kt) {
@@ -304,42 +351,36 @@ __global__ __launch_bounds__(256) void grouped_join_kernel(GroupedParams p) {
   }
 }
 
-// The same for a product with an epilogue: one thread for eight columns of one row.
+// The same for a product with an epilogue: one thread for one column of one row, whose
+// parts are loaded eight at a time (few sums are split, and short of threads).
 template <int DIR, int EPI>
 __global__ __launch_bounds__(256) void grouped_join_swiglu_kernel(GroupedParams p) {
   const int cols = columns<DIR, EPI>(p), wide = columns<DIR>(p);
-  const int units = ceil_div(cols, 8);
   const long long first = min(max(p.offsets[0], 0), p.R);
   const long long rows = min(max(p.offsets[p.E], 0), p.R);
-  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (rows - first) * units;
+  const size_t stride = (size_t)p.R * wide;
+  for (long long u = (long long)blockIdx.x * 256 + threadIdx.x; u < (rows - first) * cols;
        u += (long long)gridDim.x * 256) {
-    const long long row = first + u / units;
-    const int j = (int)(u % units) * 8, n = cols - j;
-    const float* part = static_cast<const float*>(p.part) + (size_t)row * wide + j;
-    float a[8] = {}, b[8] = {};
-    for (int s0 = 0; s0 < p.splits; s0 += 2) {
-      float x[2][8], y[2][8];
+    const size_t row = first + u / cols;
+    const int j = (int)(u % cols);
+    const float* part = static_cast<const float*>(p.part) + row * wide + j;
+    float a = 0.0f, b = 0.0f;
+    for (int s0 = 0; s0 < p.splits; s0 += 8) {
+      float x[8], y[8];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const float* at = part + (size_t)min(s0 + s, p.splits - 1) * p.R * wide;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          x[s][c] = at[min(c, n - 1)];
-          if constexpr (EPI == kSwiglu) y[s][c] = at[cols + min(c, n - 1)];
-        }
+      for (int s = 0; s < 8; ++s) {
+        const float* at = part + min(s0 + s, p.splits - 1) * stride;
+        x[s] = at[0];
+        y[s] = EPI == kSwiglu ? at[cols] : 0.0f;
       }
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int s = 0; s < 8; ++s)
         if (s0 + s < p.splits) {
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            a[c] += x[s][c];
-            if constexpr (EPI == kSwiglu) b[c] += y[s][c];
-          }
+          a += x[s];
+          b += y[s];
         }
     }
-    if constexpr (EPI == kSwiglu) store_swiglu(p, row, j, n, a, b);
-    else store_swiglu_grad(p, row, j, n, a);
+    store_one<EPI>(p, row, j, a, b);
   }
 }
 
@@ -503,7 +544,7 @@ hipError_t launch_product(GroupedParams p, const GroupedArgs& a, hipStream_t str
   if (e != hipSuccess || p.splits == 1) return e;
   const int cols = EPI == kSwiglu ? a.N / 2 : DIR == kForward ? a.N : a.K;
   const long long rows = DIR == kGradWeights ? (long long)a.E * a.N : a.R;
-  const long long blocks = (rows * ceil_div(cols, EPI == kPlain ? 4 : 8) + 255) / 256;
+  const long long blocks = (rows * ceil_div(cols, EPI == kPlain ? 4 : 1) + 255) / 256;
   const dim3 grid((unsigned)std::min<long long>(blocks, 4096)), block(256);
   // (kFp8: the parts are scaled, and join as bf16 operands' do)
   constexpr int JOIN = TYPE == kFp8 ? kBf16 : TYPE;

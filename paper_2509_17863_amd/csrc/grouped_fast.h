@@ -273,6 +273,16 @@ __device__ __forceinline__ void way_out_swiglu(const GroupedParams& p, const Gro
   const int c = (lane & (PER - 1)) * 8, n = cols - (col0 + c);
 #pragma unroll
   for (int i = 0; i < MBW; ++i) {
+    GateUp gate_up[32 / ROWS];
+    if constexpr (EPI == kSwigluGrad) {
+      if (p.splits == 1) {
+#pragma unroll
+        for (int s = 0; s < 32 / ROWS; ++s) {
+          const int ri = row0 + i * 32 + s * ROWS + lane / PER;
+          gate_up[s] = load_gate_up(p, t.i0 + ri, col0 + c, ri < t.i_valid ? n : 0);
+        }
+      }
+    }
     LDS_AS float* at = buf + lrow * LD + 4 * khalf;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -310,7 +320,7 @@ __device__ __forceinline__ void way_out_swiglu(const GroupedParams& p, const Gro
       } else if constexpr (EPI == kSwiglu) {
         store_swiglu(p, row, col0 + c, n, a, b);
       } else {
-        store_swiglu_grad(p, row, col0 + c, n, a);
+        store_swiglu_grad(p, row, col0 + c, n, gate_up[s], a, false);
       }
     }
   }

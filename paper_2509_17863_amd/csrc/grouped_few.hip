@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
       } else if constexpr (EPI == kSwiglu) {
         store_swiglu(p, row, col0, n, a, b);
       } else {
-        store_swiglu_grad(p, row, col0, n, a);
+        store_swiglu_grad(p, row, col0, n, load_gate_up(p, row, col0, n), a, false);
       }
     }
     return;

@@ -250,19 +250,7 @@ __device__ __forceinline__ void store_results(const GroupedParams& p, const Grou
 
 // Eight bf16 (n of them exist) to an address of element alignment, past the caches.
 __device__ __forceinline__ void store_far(uint16_t* at, int n, u32x4 v) {
-  typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
-  if (n >= 8) {
-    __builtin_nontemporal_store(v, reinterpret_cast<any4*>(at));
-  } else {
-#pragma unroll
-    for (int c = 0; c < 8; ++c)
-      if (c < n) at[c] = (uint16_t)(v[c / 2] >> (16 * (c & 1)));
-  }
-}
-
-__device__ __forceinline__ u32x4 to_bf16x8(const float (&v)[8]) {
-  return u32x4{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]),
-               to_bf16x2(v[6], v[7])};
+  store8_raw(at, n, v, true);
 }
 
 // kSwiglu: a wave's 128 rows x 32 columns of h, acc[i][0] gate and acc[i][1] up (layout
@@ -338,20 +326,20 @@ __device__ __forceinline__ void store_grad_results(const GroupedParams& p, const
   const int cols = p.K, col = col0 + c8 * 8, n = cols - col;
   before_stores();
   if (row0 >= t.i_valid || col0 >= cols) return;
+  // gate and up of the 16 rows that come next are on their way while 16 are stored
+  GateUp next[2];
+  auto fetch = [&](int rows16) INLINE {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const int ri = row0 + rows16 * 16 + s * 8 + m8;
+      next[s] = load_gate_up(p, t.i0 + ri, col, ri < t.i_valid ? n : 0);
+    }
+  };
+  fetch(0);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      // gate and up first: their loads are in flight while dh is passed over
-      const int ri = row0 + i * 32 + half * 16 + m8;
-      float g[2][8], u[2][8];
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int m = ri + s * 8 < t.i_valid ? n : 0;
-        const uint16_t* from = p.gu + (size_t)(t.i0 + ri + s * 8) * p.ldgu + col;
-        load8(from, m, g[s]);
-        load8(from + cols, m, u[s]);
-      }
       if ((lrow >> 4) == half) {
 #pragma unroll
         for (int j = 0; j < 2; ++j)
@@ -362,29 +350,20 @@ __device__ __forceinline__ void store_grad_results(const GroupedParams& p, const
                 f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
                       acc[i][j][4 * q + 3]};
       }
+      const GateUp here[2] = {next[0], next[1]};
+      if (2 * i + half < 7) fetch(2 * i + half + 1);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const int m = s * 8 + m8;
-        float dg[8], du[8], h[8];
+        const int m = s * 8 + m8, ri = row0 + i * 32 + half * 16 + m;
+        float d[8];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           const f32x4 v = *reinterpret_cast<const LDS_AS f32x4*>(buf + m * 256 +
                                                                  (((2 * c8 + q) ^ m) << 4));
 #pragma unroll
-          for (int c = 4 * q; c < 4 * q + 4; ++c) {
-            const SwigluGrad r = swiglu_grad(g[s][c], u[s][c], v[c - 4 * q]);
-            dg[c] = r.gate;
-            du[c] = r.up;
-            h[c] = silu_up(g[s][c], u[s][c]);
-          }
+          for (int c = 0; c < 4; ++c) d[4 * q + c] = v[c];
         }
-        if (ri + s * 8 < t.i_valid) {
-          const size_t row = t.i0 + ri + s * 8;
-          uint16_t* to = static_cast<uint16_t*>(p.out) + row * p.ldo + col;
-          store_far(to, n, to_bf16x8(dg));
-          store_far(to + cols, n, to_bf16x8(du));
-          if (p.h) store_far(p.h + row * p.ldh + col, n, to_bf16x8(h));
-        }
+        if (ri < t.i_valid) store_swiglu_grad(p, t.i0 + ri, col, n, here[s], d, true);
       }
     }
   }

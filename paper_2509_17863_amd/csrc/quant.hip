@@ -90,7 +90,14 @@ __device__ __forceinline__ void load_values(const void* x, long long at, int n, 
       __builtin_memcpy(v, p, 32);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+      if (n > 0) {
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = p[min(i, n - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? e[i] : 0.0f;
+      }
     }
   } else {
     load8(static_cast<const uint16_t*>(x) + at, n, v);

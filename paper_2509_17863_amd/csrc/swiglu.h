@@ -17,9 +17,17 @@ __device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
       v[2 * i] = __uint_as_float(raw[i] << 16);
       v[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
     }
+  } else if (n > 0) {
+    // (every element is loaded, the last one repeatedly: loads under a condition each would
+    // be waited for one by one)
+    uint32_t e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = p[min(i, n - 1)];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? __uint_as_float(e[i] << 16) : 0.0f;
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? __uint_as_float((uint32_t)p[i] << 16) : 0.0f;
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
   }
 }
 
