@@ -72,9 +72,10 @@ __device__ __forceinline__ u32x4 shift_down(u32x4 v, int n) {
 //   ACROSS: rows are the sum's index [s0, s0 + 64) up to s_end, columns
 //           [c0, c0 + 128) of `width`
 //   else:   128 rows (pointers fixed for the whole sum), 128 bytes of the sum
-//   TOGETHER: how tiles along an edge are loaded (dW, whose operands both lie across and
-//   whose sums are often shorter than a tile, keeps loads that nothing needs out: 4 rows
-//   an expert 157 us against 170; 8-bit integers have no registers left for the shift)
+//   TOGETHER: how tiles along an edge are loaded.  (The operand across the sum in dx alone:
+//   every tile of an edge's columns ends inside.  Along the sum only the last one does, and
+//   with codes the shift's registers cost more; in dW, whose sums are often shorter than a
+//   tile, it loads what nothing needs, 4 rows an expert 157 us against 170.)
 template <bool ACROSS, int ESZ, bool TOGETHER>
 struct Loader {
   static constexpr int EPC = 16 / ESZ;  // elements of a chunk
@@ -210,9 +211,8 @@ void grouped_any_kernel(GroupedParams p) {
         src[q] = source_row(p, min(t.beg + kt * SUM + (int)threadIdx.x / 16 + 16 * q, t.end - 1));
     }
   };
-  constexpr bool TOGETHER = DIR != kGradWeights && !I8;
-  Loader<A_ACROSS, ESZ, TOGETHER> la;
-  Loader<B_ACROSS, ESZ, TOGETHER> lb;
+  Loader<A_ACROSS, ESZ, false> la;
+  Loader<B_ACROSS, ESZ, DIR == kGradRows> lb;
   la.init(a_row);
   lb.init(b_row);
   auto load = [&](int kt) {

@@ -40,9 +40,12 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
   constexpr int ESZ = TYPE == kBf16 ? 2 : 1, SUM = 128 / ESZ;
   constexpr int BI = 16 * MB, NB = kJ / 16;
   constexpr int kOutJ = EPI == kSwiglu ? kJ / 2 : kJ;  // columns of a result tile
-  constexpr int kXBytes = BI * 128, kSBytes = FP8 ? 256 : 0, kStage = kWBytes + kXBytes + kSBytes;
+  // kFp8: the rows' scales travel in the stage, or, where they would keep a second workgroup
+  // off the CU, in a register: four tiles' at a time, one for each quarter of the wave
+  constexpr bool S_STAGE = FP8 && MB > 1, S_REG = FP8 && MB == 1;
+  constexpr int kXBytes = BI * 128, kSBytes = S_STAGE ? 256 : 0, kStage = kWBytes + kXBytes + kSBytes;
   constexpr int W_INST = kWBytes / 1024, X_INST = kXBytes / 1024;
-  constexpr int INST = W_INST + X_INST + (FP8 ? 1 : 0);
+  constexpr int INST = W_INST + X_INST + (S_STAGE ? 1 : 0);
   constexpr int LD = kJ + 4;
   constexpr int kRing = kWaves * STAGES * kStage, kParts = kWaves * BI * LD * 4;
   __shared__ __attribute__((aligned(1024))) char smem_raw[kRing > kParts ? kRing : kParts];
@@ -92,11 +95,18 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
   const char* s_base = nullptr;
   uint32_t s_bytes = 0, s_off = 0;
   const CONST_AS float* col_scale = nullptr;
-  if constexpr (FP8) {
+  const float* row_scale = nullptr;
+  if constexpr (S_REG) {
+    const int row = min(lane & 15, t.i_valid - 1);
+    row_scale = p.row_scale + (size_t)source_row(p, t.i0 + row) * kb;
+  }
+  if constexpr (S_STAGE) {
     const int row = min(lane, t.i_valid - 1);
     s_base = reinterpret_cast<const char*>(p.row_scale + (gather ? 0 : (size_t)t.i0 * kb));
     s_bytes = (uint32_t)((gather ? p.R / p.k : t.i_valid) * 4LL * kb);
     s_off = (uint32_t)((gather ? source_row(p, t.i0 + row) : row) * 4LL * kb);
+  }
+  if constexpr (FP8) {
     col_scale = (const CONST_AS float*)(p.col_scale +
                                         ((size_t)t.e * ceil_div(p.N, 128) + t.j0 / 128) * kb);
   }
@@ -131,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
 #pragma unroll
     for (int q = 0; q < X_INST; ++q)
       load_lds16(d, (q & 1 ? odd : even) ? x_off[q] : kNowhere, dst + kWBytes + q * 1024);
-    if constexpr (FP8)
+    if constexpr (S_STAGE)
       load_lds4(descriptor(s_base + (size_t)at * 4, s_bytes - (uint32_t)at * 4), s_off,
                 dst + kWBytes + kXBytes);
   };
@@ -216,8 +226,9 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
     if constexpr (FP8) {
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
-        const float f = col * *reinterpret_cast<const LDS_AS float*>(stage + kWBytes + kXBytes +
-                                                                     (i * 16 + l16) * 4);
+        float f = col;
+        if constexpr (S_STAGE)
+          f *= *reinterpret_cast<const LDS_AS float*>(stage + kWBytes + kXBytes + (i * 16 + l16) * 4);
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -230,13 +241,22 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
   for (int s = 0; s < STAGES; ++s)
     if (s < nk) issue(s);
   float col = FP8 && nk > 0 ? col_scale[first] : 0.0f;
+  // (a load that the compiler waits for waits for the ring as well: once in four tiles)
+  float four = 0.0f, coming = S_REG && nk > 0 ? row_scale[min(first + g, kb - 1)] : 0.0f;
   for (int kt = 0; kt < nk; ++kt) {
+    if constexpr (S_REG) {
+      if ((kt & 3) == 0) {
+        four = coming;
+        if (kt + 4 < nk) coming = row_scale[min(first + kt + 4 + g, kb - 1)];
+      }
+    }
     const float next = FP8 ? col_scale[first + min(kt + 1, nk - 1)] : 0.0f;
     // (past the last full ring the count is not known here: wait for all)
     if (kt + STAGES <= nk) wait_vmcnt<(STAGES - 1) * INST>();
     else wait_vmcnt<0>();
     asm volatile("" ::: "memory");
-    multiply(ring + (kt % STAGES) * kStage, col);
+    multiply(ring + (kt % STAGES) * kStage,
+             S_REG ? col * __shfl(four, (kt & 3) * 16 + l16, kWave) : col);
     col = next;
     // the stage is read: it may be filled again
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -329,8 +349,7 @@ template <int DIR, int TYPE, int EPI>
 hipError_t launch_grouped_few(const GroupedParams& p, int rows, long long tiles,
                               hipStream_t stream) {
   if (tiles > 0x7fffffffLL) return hipErrorInvalidValue;
-  // (kFp8: with the rows' scales two workgroups of 16 rows no longer fit a CU)
-  if (rows == 16) return launch<DIR, TYPE, EPI, 1, TYPE == kFp8 ? 3 : 2>(p, tiles, stream);
+  if (rows == 16) return launch<DIR, TYPE, EPI, 1, 2>(p, tiles, stream);
   if (rows == 32) return launch<DIR, TYPE, EPI, 2, 3>(p, tiles, stream);
   return launch<DIR, TYPE, EPI, 4, 2>(p, tiles, stream);
 }
