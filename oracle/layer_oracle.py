@@ -145,7 +145,7 @@ def e4m3_codes(x):
 
 def quantize_blocks(x, block_rows=1):
     """(codes, scales) of an fp32 matrix: a scale for each block of block_rows x 128,
-    amax / 448 in fp32 (1 where that is zero), quotients in fp32; NaN and zero codes for a
+    amax * fp32(1/448) (1 where that is zero), quotients in fp32; NaN and zero codes for a
     block that holds an infinity or a NaN."""
     x = np.asarray(x, np.float32)
     n, K = x.shape
@@ -158,7 +158,7 @@ def quantize_blocks(x, block_rows=1):
             if not np.isfinite(b).all():
                 s[i, j] = np.nan
                 continue
-            sc = np.float32(np.abs(b).max() / np.float32(448))
+            sc = np.float32(np.abs(b).max() * np.float32(1 / 448))
             s[i, j] = np.float32(1) if sc == 0 else sc
             q[at] = e4m3_codes(b / s[i, j])
     return q, s

@@ -16,9 +16,16 @@
 //   group 0, phase 2t:   M(t): load A tile t+1 and its rows' scales, fragments of tile t
 //   group 0, phase 2t+1: C(t), then wait until A tile t+1 has landed
 //   group 1, phase 2t+1: M(t): fragments of tile t, wait until B tile t+1 has landed
-//   group 1, phase 2t+2: C(t), with the loads of B tile t+2 among its first instructions
+//   group 1, phase 2t+2: C(t), with the loads of B tile t+2 spread among its instructions
 // Both operands have two LDS stages: group 1 loads in its C phase, when the stage that tile
-// t had is free, so no third one is needed, and the scales and the way out have room.
+// t had is free, so no third one is needed, and the scales and the way out have room.  A
+// row's scales for four tiles are one load of 16 bytes where rows of scales allow it.
+//
+// 32768 rows of 32 experts, 4096 x 7168: 0.89 ms, 2.17 PFLOP/s; 8192^3: 0.49 ms, 2.25 (the
+// loads of B ahead of C's first instruction: 0.92; and scales one at a time: 1.07).  Without
+// loads the loop takes 0.64: what bounds it is their latency, which two stages cover by two
+// phases.  Five half stages of B with all loads in M phases, half of them a phase earlier,
+// took 0.87, but 0.52 ms instead of 0.49 where K is 2048.
 #include "grouped_pp.h"
 
 namespace eaas {
@@ -26,8 +33,8 @@ namespace {
 
 #define INLINE __attribute__((always_inline))
 
-constexpr int kScales = 4 * kStage;            // LDS: rows' scales, two stages of 1 KiB
-constexpr int kOffsets = kScales + 2 * 1024;   // gathered rows' offsets
+constexpr int kScales = 4 * kStage;            // LDS: rows' scales, two stages of 4 KiB
+constexpr int kOffsets = kScales + 2 * 4096;   // gathered rows' offsets
 constexpr int kOut = kOffsets + 1024;          // 2 KiB for each wave's way out
 constexpr int kFp8Lds = kOut + 8 * 2048;
 
@@ -62,8 +69,8 @@ __device__ __forceinline__ void store_fp8_results(const GroupedParams& p, const 
   }
 }
 
-// GATHER: rows of x come through perm.
-template <bool GATHER>
+// GATHER: rows of x come through perm.  QUADS: rows of scales in multiples of 16 bytes.
+template <bool GATHER, bool QUADS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void grouped_fp8_kernel(GroupedParams p) {
   __shared__ __attribute__((aligned(1024))) char smem_raw[kFp8Lds];
@@ -121,25 +128,35 @@ void grouped_fp8_kernel(GroupedParams p) {
     }
     off0 = (uint32_t)((w4 * 8 + (lane >> 3)) * p.K) + my_chunk * 16;
   };
-  auto issue = [&](int kt) INLINE {
+  // What loads instruction q of tile kt; past the last tile, zeros (from nowhere: the
+  // descriptor stays that of the last one).
+  auto loads = [&](int kt) INLINE {
     const uint32_t lds = opaque(lds0 + (grp * 2 + (kt & 1)) * kStage);
     const uint32_t step = opaque((uint32_t)p.K * 32);
-    const i32x4 d = descriptor(base + (size_t)kt * 128, bytes - (uint32_t)kt * 128);
+    const int from = min(kt, nk - 1) * 128;
+    const i32x4 d = descriptor(base + from, bytes - (uint32_t)from);
     const bool in = kt * 8 + my_chunk < chunks;
-    if (GATHER && grp == 0) {
-      const LDS_AS char* at = smem + kOffsets + (w4 * 64 + (lane >> 3)) * 4;
+    auto one = [=](int q) INLINE {
+      uint32_t off = off0 + q * step;
+      if (GATHER && grp == 0)
+        off = *reinterpret_cast<const LDS_AS uint32_t*>(smem + kOffsets + (w4 * 64 + (lane >> 3)) * 4 +
+                                                        q * 32) + my_chunk * 16;
+      load_lds16(d, in ? off : kNowhere, lds + (w4 + 4 * q) * 1024);
+    };
+    return one;
+  };
+  auto issue = [&](int kt) INLINE {
+    auto one = loads(kt);
 #pragma unroll
-      for (int q = 0; q < kInst; ++q)
-        load_lds16(d, in ? *reinterpret_cast<const LDS_AS uint32_t*>(at + q * 32) + my_chunk * 16
-                         : kNowhere, lds + (w4 + 4 * q) * 1024);
-    } else {
-#pragma unroll
-      for (int q = 0; q < kInst; ++q)
-        load_lds16(d, in ? off0 + q * step : kNowhere, lds + (w4 + 4 * q) * 1024);
+    for (int q = 0; q < kInst; ++q) one(q);
+    if (grp == 0) {
+      const i32x4 d = descriptor(s_base + (size_t)kt * 4, s_bytes - (uint32_t)kt * 4);
+      if constexpr (QUADS) {
+        if ((kt & 3) == 0) load_lds16(d, s_off, opaque(lds0 + kScales + (kt & 4) * 1024) + w4 * 1024);
+      } else {
+        load_lds4(d, s_off, opaque(lds0 + kScales + (kt & 1) * 4096) + w4 * 256);
+      }
     }
-    if (grp == 0)
-      load_lds4(descriptor(s_base + (size_t)kt * 4, s_bytes - (uint32_t)kt * 4), s_off,
-                opaque(lds0 + kScales + (kt & 1) * 1024) + w4 * 256);
   };
 
   // fragments: lane l holds row or column l % 16 of a block and 32 bytes of the sum, the
@@ -162,7 +179,9 @@ void grouped_fp8_kernel(GroupedParams p) {
   auto load_frags = [&](auto mb, int kt, Frags& f) INLINE {
     const LDS_AS char* sa = smem + (kt & 1) * kStage + grp * 128 * 128;
     const LDS_AS char* sb = smem + (2 + (kt & 1)) * kStage + w4 * 64 * 128;
-    const LDS_AS char* sc = smem + kScales + (kt & 1) * 1024 + (grp * 128 + l16) * 4;
+    constexpr int PITCH = QUADS ? 16 : 4;  // bytes between the scales of two rows
+    const LDS_AS char* sc = smem + kScales + (grp * 128 + l16) * PITCH +
+                            (QUADS ? (kt & 4) * 1024 + (kt & 3) * 4 : (kt & 1) * 4096);
     int at = at16;
     asm volatile("" : "+v"(at));
 #pragma unroll
@@ -171,7 +190,7 @@ void grouped_fp8_kernel(GroupedParams p) {
 #pragma unroll
     for (int i = 0; i < decltype(mb)::value; ++i) {
       f.a[i] = fragment(sa + i * 2048, at);
-      f.f[i] = *reinterpret_cast<const LDS_AS float*>(sc + i * 64) * col;
+      f.f[i] = *reinterpret_cast<const LDS_AS float*>(sc + i * 16 * PITCH) * col;
     }
     // the stages may be filled again behind the next barriers
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -179,12 +198,14 @@ void grouped_fp8_kernel(GroupedParams p) {
   // One instruction for each 16 x 16 block, whose sums are added three blocks later: by then
   // they are there (one behind costs 90% more time than the instructions alone, two 30%,
   // three 14%).
-  auto mfmas = [&](auto mb, const Frags& f) INLINE {
-    constexpr int BLOCKS = decltype(mb)::value * 4, BEHIND = 3;
+  // between(q), q = 0 .. 7: called among them.
+  auto mfmas = [&](auto mb, const Frags& f, auto between) INLINE {
+    constexpr int BLOCKS = decltype(mb)::value * 4, BEHIND = 3, EVERY = BLOCKS / kInst;
     __builtin_amdgcn_s_setprio(1);
     f32x4 part[BEHIND + 1];
 #pragma unroll
     for (int n = 0; n < BLOCKS + BEHIND; ++n) {
+      if (n < BLOCKS && n % EVERY == EVERY - 1) between(n / EVERY);
       if (n < BLOCKS)
         part[n % (BEHIND + 1)] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
             f.b[n % 4], f.a[n / 4], f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0);
@@ -212,6 +233,7 @@ void grouped_fp8_kernel(GroupedParams p) {
   };
   auto walk = [&](auto mb) INLINE {
     constexpr bool LIVE = decltype(mb)::value > 0;
+    auto nothing = [](int) {};
     if (grp == 0) {
 #pragma unroll 1
       for (int kt = 0; kt < nk; ++kt) {
@@ -219,7 +241,7 @@ void grouped_fp8_kernel(GroupedParams p) {
         Frags f;
         if constexpr (LIVE) load_frags(mb, kt, f);
         phase_end();
-        if constexpr (LIVE) mfmas(mb, f);
+        if constexpr (LIVE) mfmas(mb, f, nothing);
         if (kt >= 1) wait_vmcnt<0>();
         phase_end();
       }
@@ -231,10 +253,11 @@ void grouped_fp8_kernel(GroupedParams p) {
         if constexpr (LIVE) load_frags(mb, kt, f);
         wait_vmcnt<0>();
         phase_end();
-        if (kt + 2 < nk) issue(kt + 2);
-        if constexpr (LIVE) mfmas(mb, f);
+        if constexpr (LIVE) mfmas(mb, f, loads(kt + 2));
+        else issue(kt + 2);
         if (kt + 1 < nk) phase_end();
       }
+      wait_vmcnt<0>();  // (the zeros are there: the next results' tiles go where they went)
     }
   };
 
@@ -380,11 +403,13 @@ hipError_t launch_grouped_fp8_pp(const GroupedParams& p, long long tiles, hipStr
   if (e != hipSuccess) return e;
   // one workgroup to a CU
   const dim3 grid((unsigned)std::min<long long>(tiles, 256)), block(kThreads);
-  if (p.perm)
-    hipLaunchKernelGGL(grouped_fp8_kernel<true>, grid, block, 0, stream, p);
-  else
-    hipLaunchKernelGGL(grouped_fp8_kernel<false>, grid, block, 0, stream, p);
-  return hipGetLastError();
+  const bool quads = ceil_div(p.K, 128) % 4 == 0 && (uintptr_t)p.row_scale % 16 == 0;
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, p);
+    return hipGetLastError();
+  };
+  if (p.perm) return quads ? go(grouped_fp8_kernel<true, true>) : go(grouped_fp8_kernel<true, false>);
+  return quads ? go(grouped_fp8_kernel<false, true>) : go(grouped_fp8_kernel<false, false>);
 }
 
 }  // namespace eaas

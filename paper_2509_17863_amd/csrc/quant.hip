@@ -60,11 +60,12 @@ __device__ __forceinline__ uint32_t largest16(uint32_t m) {
   return m;
 }
 
-// The scale of a block: its largest magnitude / 448, or 1 where that is zero (a block of
-// zeros, or below 448 times fp32's least); NaN if the block holds an infinity or a NaN.
+// The scale of a block: its largest magnitude times 1/448 rounded to fp32, or 1 where that
+// is zero (a block of zeros, or next to fp32's least); NaN if the block holds an infinity or
+// a NaN.
 __device__ __forceinline__ float block_scale(uint32_t m) {
   if (m >= 0x7f800000u) return __uint_as_float(0x7fc00000u);
-  const float s = __uint_as_float(m) / 448.0f;
+  const float s = __uint_as_float(m) * (1.0f / 448.0f);
   return s == 0.0f ? 1.0f : s;
 }
 

@@ -37,7 +37,7 @@ def test_blocks(n, K, block_rows):
     assert (np.abs(d - x) <= np.maximum(np.abs(x) * 2.0 ** -4, full * 2.0 ** -10) * 1.0001).all()
     for i in range(s.shape[0]):
         b = np.abs(x[i * block_rows: (i + 1) * block_rows, :128]).max()
-        assert s[i, 0] == (np.float32(b) / np.float32(448) if b else 1)
+        assert s[i, 0] == (np.float32(b) * np.float32(1 / 448) if b else 1)
 
 
 def test_blocks_of_zeros_and_of_no_numbers():

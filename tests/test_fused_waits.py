@@ -8,8 +8,9 @@ from test_grouped_waits import under_way_at_barriers
 
 from paper_2509_17863_amd import _build
 
-# (source, kernel, how many of it): gathered or not, and the way back; gathered or not
-KERNELS = [("grouped_swiglu.hip", "grouped_pp_kernel", 3), ("grouped_fp8.hip", "grouped_fp8_kernel", 2),
+# (source, kernel, how many of it): gathered or not, and the way back; gathered or not, with
+# rows of scales in multiples of 16 bytes or not
+KERNELS = [("grouped_swiglu.hip", "grouped_pp_kernel", 3), ("grouped_fp8.hip", "grouped_fp8_kernel", 4),
            ("grouped_fp8.hip", "grouped_fp8_mid_kernel", 1)]
 
 

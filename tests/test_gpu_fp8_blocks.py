@@ -49,13 +49,17 @@ def test_rows(gpu, rows, K, pad, dtype):
     assert (flat[rows * K:] == 77).all()
 
 
-def test_rows_equal_the_step_s_own_quantizer(gpu):
+def test_rows_beside_the_step_s_own_quantizer(gpu):
+    """That one divides by 448: scales a unit in the last place apart at most, codes one."""
     x = values((333, 1024), 3).cuda()
     q, s = torch.empty((333, 1024), dtype=torch.uint8, device="cuda"), torch.empty((333, 8), device="cuda")
     q2, s2 = torch.empty_like(q).view(torch.float8_e4m3fn), torch.empty_like(s)
     eaas.eaas_quantize_rows_fp8(x, q, s)
     eaas.eaas_quantize_blocks_fp8(x, q2, s2)
-    assert torch.equal(q, q2.view(torch.uint8)) and torch.equal(s, s2)
+    assert ((s - s2).abs() <= 2.0 ** -23 * s).all()
+    same = (s == s2).repeat_interleave(128, 1)
+    q2 = q2.view(torch.uint8)
+    assert torch.equal(q[same], q2[same]) and ((q.int() - q2.int()).abs() <= 1).all()
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
@@ -116,7 +120,7 @@ def test_swiglu_rows_on_millions_of_values(gpu):
     s = torch.empty((8192, 6), device="cuda")
     eaas.eaas_swiglu_fp8(gu.cuda(), q, s)
     h = torch.from_numpy(silu_up(gu)).view(8192, 6, 128)
-    ws = h.abs().amax(2) / 448.0
+    ws = h.abs().amax(2) * torch.tensor(1 / 448, dtype=torch.float32)
     assert torch.equal(s.cpu(), ws)
     want = (h / ws[:, :, None]).to(torch.float8_e4m3fn).view(8192, 768)
     assert torch.equal(q.cpu().view(torch.uint8), want.view(torch.uint8))
