@@ -1,11 +1,11 @@
-"""An expert layer trained and then served in 8-bit integers, on the library's
-separate products.
+"""An expert layer trained and then served in 8 bits, on the library's separate
+products.
 
     python examples/expert_layer.py
 
 fits the experts of a small layer to another layer's outputs (fp32 master weights,
 gradients of two micro-batches added up), then quantizes the trained experts and
-serves the same tokens with 8-bit products.
+serves the same tokens with products of 8-bit integers and of block-scaled e4m3.
 
 The layer is the one of eaas_expert_forward: a token's k slots name experts (ids of
 experts that live elsewhere are skipped), every expert is the SwiGLU form without
@@ -78,6 +78,76 @@ class ExpertLayer:
         eaas.eaas_unpermute_combine(self.dx_rows, r, self.ones, dx, self.E, I=self.I)
 
 
+class FusedExpertLayer(ExpertLayer):
+    """The same layer with the activation inside the products: the gated half is one call,
+    and so is its way back, which leaves h to be computed there again instead of kept."""
+
+    def forward(self, x, ids, scores, w_gate_up, w_down, out):
+        r = self.routing
+        eaas.eaas_route_permute(ids, self.E, r, self.route_ws, H=self.H, I=self.I)
+        self.off = r["offsets"]
+        self.x, self.scores, self.w_gate_up, self.w_down = x, scores, w_gate_up, w_down
+        eaas.eaas_grouped_swiglu(x, self.off, w_gate_up, self.h, self.ws, gu=self.gate_up,
+                                 perm=r["perm"], k=self.k)
+        eaas.eaas_grouped_matmul(self.h, self.off, w_down, self.y, self.ws)
+        eaas.eaas_unpermute_combine(self.y, r, scores, out, self.E, I=self.I)
+
+    def backward(self, dout, dx, dscores, dw_gate_up, dw_down, accumulate=False):
+        r = self.routing
+        eaas.eaas_unpermute_combine_backward(dout, self.y, r, self.scores, self.dy, dscores,
+                                             self.E, I=self.I)
+        eaas.eaas_grouped_swiglu_backward(self.dy, self.off, self.w_down, self.gate_up,
+                                          self.dgate_up, self.ws, h=self.h)
+        eaas.eaas_grouped_matmul_dw(self.dy, self.h, self.off, dw_down, self.ws,
+                                    accumulate=accumulate)
+        eaas.eaas_grouped_matmul_dw(self.dgate_up, self.x, self.off, dw_gate_up, self.ws,
+                                    perm=r["perm"], k=self.k, accumulate=accumulate)
+        eaas.eaas_grouped_matmul_dx(self.dgate_up, self.off, self.w_gate_up, self.dx_rows, self.ws)
+        eaas.eaas_unpermute_combine(self.dx_rows, r, self.ones, dx, self.E, I=self.I)
+
+
+class Fp8Experts:
+    """The experts in e4m3: weights with a scale for each block of 128 x 128, quantized
+    once; activations with a scale for each 128 columns of a row, quantized on the way."""
+
+    def __init__(self, T, k, w_gate_up, w_down):
+        self.E, two_i, self.H = w_gate_up.shape
+        self.T, self.k, self.I = T, k, two_i // 2
+        R, hb, ib = T * k, (self.H + 127) // 128, (self.I + 127) // 128
+        self.gate_up_q, self.gate_up_s = self._weights(w_gate_up)
+        self.down_q, self.down_s = self._weights(w_down)
+        self.routing = eaas.alloc_routing(T, k, self.E)
+        self.route_ws = eaas.alloc_workspace(T, self.H, self.I, self.E, k)
+        n = max(eaas.eaas_grouped_fp8_workspace_bytes(R, self.E, two_i, self.H),
+                eaas.eaas_grouped_fp8_workspace_bytes(R, self.E, self.H, self.I))
+        self.ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        e4m3 = torch.float8_e4m3fn
+        self.xq, self.xs = _buf(T, self.H, dtype=e4m3), _buf(T, hb, dtype=torch.float32)
+        self.gate_up = _buf(R, two_i)
+        self.hq, self.hs = _buf(R, self.I, dtype=e4m3), _buf(R, ib, dtype=torch.float32)
+        self.y = _buf(R, self.H, dtype=torch.float32)
+
+    @staticmethod
+    def _weights(w):
+        E, N, K = w.shape
+        q = _buf(E, N, K, dtype=torch.float8_e4m3fn)
+        s = _buf(E, (N + 127) // 128, (K + 127) // 128, dtype=torch.float32)
+        eaas.eaas_quantize_blocks_fp8(w, q, s)
+        return q, s
+
+    def forward(self, x, ids, scores, out):
+        r = self.routing
+        eaas.eaas_route_permute(ids, self.E, r, self.route_ws, H=self.H, I=self.I)
+        off = r["offsets"]
+        eaas.eaas_quantize_blocks_fp8(x, self.xq, self.xs)
+        eaas.eaas_grouped_matmul_fp8(self.xq, self.xs, off, self.gate_up_q, self.gate_up_s,
+                                     self.gate_up, self.ws, perm=r["perm"], k=self.k)
+        eaas.eaas_swiglu_fp8(self.gate_up, self.hq, self.hs, n_rows=off[self.E:])
+        eaas.eaas_grouped_matmul_fp8(self.hq, self.hs, off, self.down_q, self.down_s, self.y,
+                                     self.ws)
+        eaas.eaas_unpermute_combine(self.y, r, scores, out, self.E, I=self.I)
+
+
 class Int8Experts:
     """The experts in 8-bit integers: weights with a scale per output channel,
     quantized once; activations with a scale per row, quantized on the way."""
@@ -131,10 +201,10 @@ def weights(E, H, I, gen):
     return make(E, 2 * I, H), make(E, H, I)
 
 
-def train(steps=30, T=512, H=256, I=128, E=8, k=2, lr=64.0, seed=0):
+def train(steps=30, T=512, H=256, I=128, E=8, k=2, lr=64.0, seed=0, make=ExpertLayer):
     """Losses of the steps, and the trained experts (bf16) with a batch."""
     gen = torch.Generator(device="cuda").manual_seed(seed)
-    layer = ExpertLayer(T, H, I, E, k)
+    layer = make(T, H, I, E, k)
     target = [w.to(torch.bfloat16) for w in weights(E, H, I, gen)]
     master = [t.float() + 0.5 * w for t, w in zip(target, weights(E, H, I, gen))]
     grads = [torch.empty_like(m) for m in master]
@@ -158,14 +228,15 @@ def train(steps=30, T=512, H=256, I=128, E=8, k=2, lr=64.0, seed=0):
 
 
 def main():
-    losses, w, b, layer = train()
+    losses, w, b, layer = train(make=FusedExpertLayer)
     print("loss", " ".join(f"{v:.4f}" for v in losses[::5] + losses[-1:]))
     T, H = b[0].shape
     out, served = _buf(T, H, dtype=torch.float32), _buf(T, H, dtype=torch.float32)
     layer.forward(*b, *w, out)
-    Int8Experts(T, layer.k, *w).forward(*b, served)
-    rel = ((served - out).norm() / out.norm()).item()
-    print(f"8-bit experts: {rel:.4f} of the outputs' norm from the bf16 layer")
+    for name, experts in (("8-bit integer", Int8Experts), ("e4m3", Fp8Experts)):
+        experts(T, layer.k, *w).forward(*b, served)
+        rel = ((served - out).norm() / out.norm()).item()
+        print(f"{name} experts: {rel:.4f} of the outputs' norm from the bf16 layer")
 
 
 if __name__ == "__main__":

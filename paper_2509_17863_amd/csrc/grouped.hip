@@ -499,10 +499,25 @@ GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   const int some = a.dir == kForward && a.type == kBf16 ? 48 : 16;
   if (has_large && rows >= some && large >= 192 && steps >= 4) return on_large;
   GroupedPlan few{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};
-  const double cells = (double)out_tiles(a, few.bi, few.bj);
   double t_few;
-  few.splits = best_parts(steps, out, [&](int s) { return few_us(cells, steps, few.bi, s); },
-                          &t_few);
+  auto estimate = [&](GroupedPlan& g, double* time) {
+    const double cells = (double)out_tiles(a, g.bi, g.bj);
+    // (64 rows of codes take longer to convert than their weights to load)
+    const double slow = a.type == kFp8 && g.bi == 64 ? 1.3 : 1;
+    g.splits = best_parts(steps, out, [&](int s) { return slow * few_us(cells, steps, g.bi, s); },
+                          time);
+  };
+  estimate(few, &t_few);
+  // e4m3 and products with an epilogue: smaller tiles too, where few columns leave CUs idle
+  // (110 rows x 2, 1728 x 4048, e4m3: 17.6 on 64 rows, 12.7 on 16)
+  if (a.type == kFp8 || a.epilogue != kPlain) {
+    for (int bi = 16; bi < few.bi; bi *= 2) {
+      GroupedPlan g{kFew, bi, 64, 1};
+      double t;
+      estimate(g, &t);
+      if (t < t_few) few = g, t_few = t;
+    }
+  }
   if (rows <= 24 && steps >= 4) return few;
   const double t_large = large_us((double)large, steps);
   return has_large && t_large < std::min(t_any, t_few) ? on_large : t_few < t_any ? few : any;

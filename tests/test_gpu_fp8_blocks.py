@@ -278,7 +278,8 @@ def test_codes_from_any_byte(gpu, shape, dtype):
 EXACT = [(5, 1, 40, 70000, "one", 0), (20, 2, 96, 4096, "some", 4), (64, 1, 64, 8192, "even", 0),
          (200, 2, 264, 9008, "one", 4), (9, 2, 33, 30001, "even", 3), (512, 16, 1024, 2048, "ragged", 2),
          (3000, 5, 6200, 528, "ragged", 0), (3000, 4, 6201, 1040, "some", 4),
-         (2600, 5, 6144, 1300, "ragged", 0)]
+         (2600, 5, 6144, 1300, "ragged", 0), (13, 1, 32, 448, "even", 0), (19, 1, 224, 6080, "even", 0),
+         (32, 1, 12256, 2192, "one", 4), (300, 7, 136, 64, "some", 3), (839, 1, 2048, 2592, "one", 0)]
 
 
 def test_every_kernel_is_among_these():
@@ -287,9 +288,12 @@ def test_every_kernel_is_among_these():
     for R, E, N, K, *_ in EXACT:
         for product in ("fp8", "fp8_fp32"):
             kernel, rows, parts = eaas._grouped_plan(product, R, E, N, K, K % 16 == 0)
-            seen.add((product, kernel, rows if kernel == "few" else 0, parts > 1))
-    for want in [("fp8", "large", 0, False), ("fp8", "any", 0, False), ("fp8", "any", 0, True),
-                 ("fp8", "few", 16, True), ("fp8", "few", 64, True), ("fp8", "few", 64, False)]:
+            seen.add((product, K % 16 == 0, kernel, rows if kernel == "few" else 0, parts > 1))
+    for want in [("fp8", True, "large", 0, False), ("fp8", True, "any", 0, False),
+                 ("fp8", True, "any", 0, True), ("fp8", False, "any", 0, False),
+                 ("fp8", False, "any", 0, True), ("fp8", True, "few", 16, False),
+                 ("fp8", True, "few", 16, True), ("fp8", True, "few", 32, False),
+                 ("fp8", True, "few", 32, True), ("fp8", True, "few", 64, False)]:
         assert want in seen, (want, seen)
 
 

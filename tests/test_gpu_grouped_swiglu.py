@@ -199,7 +199,27 @@ def test_backward(gpu, shape, mode):
 
 WHOLE = [(5, 1, 40, 9000, "one", 0), (20, 2, 96, 1024, "some", 4), (64, 1, 64, 2048, "even", 0),
          (9, 2, 33, 3001, "even", 3), (512, 16, 512, 512, "ragged", 2), (3000, 5, 3500, 264, "ragged", 0),
-         (3000, 4, 3501, 264, "some", 4), (2600, 5, 3080, 392, "ragged", 0)]
+         (3000, 4, 3501, 264, "some", 4), (2600, 5, 3080, 392, "ragged", 0),
+         (13, 1, 16, 2992, "even", 0), (263, 1, 160, 5232, "one", 0), (18, 1, 40, 176, "even", 3),
+         (2981, 1, 496, 1808, "even", 0), (17, 1, 16, 3328, "even", 0), (362, 1, 272, 4320, "one", 0),
+         (2002, 1, 1632, 1760, "even", 0), (130, 3, 65, 65, "ragged", 0)]
+
+
+def test_every_kernel_is_among_these():
+    """On the host: every way of computing either, in one part and in several."""
+    for way in ("swiglu", "swiglu_backward"):
+        seen = set()
+        for R, E, I, wide, *_ in WHOLE:
+            N, K = (2 * I, wide) if way == "swiglu" else (wide, I)
+            in16 = K % 8 == 0 and (way == "swiglu" or N % 8 == 0)
+            kernel, rows, parts = eaas._grouped_plan(way, R, E, N, K, in16)
+            seen.add((in16, kernel, rows if kernel == "few" else 0, parts > 1))
+        for want in [(True, "large", 0, False), (True, "any", 0, True), (False, "any", 0, False),
+                     (False, "any", 0, True), (True, "few", 16, False), (True, "few", 16, True),
+                     (True, "few", 32, False), (True, "few", 32, True), (True, "few", 64, False),
+                     (True, "few", 64, True)]:
+            assert want in seen, (way, want, seen)
+
 
 
 @pytest.mark.parametrize("shape", WHOLE, ids=str)
@@ -210,6 +230,7 @@ def test_sums_that_are_exact_in_any_order(gpu, shape):
     h, gu, want = c.forward()
     assert np.array_equal(gu.values(c.live), rounded(want[1]).double().numpy())
     check_forward(c, h, gu, want)
+    check_backward(c, *c.backward())
 
 
 @pytest.mark.parametrize("shape", [(64, 1, 64, 2048, "even", 0), (3000, 5, 6200, 264, "ragged", 0),
