@@ -84,10 +84,6 @@ __device__ __forceinline__ float silu_far_up(float g, float up) {
   return (g * z) * (z * up);
 }
 
-__device__ __forceinline__ float silu_full_up(float g, float up) {
-  return g < kFar ? silu_far_up(g, up) : silu_full(g) * up;
-}
-
 // The gradient of a gate and its up value from that of h, and h itself.
 struct SwigluGrad {
   float gate, up;

@@ -306,18 +306,21 @@ def test_sums_that_are_exact_in_any_order(gpu, shape, dtype):
     assert torch.equal(c.run(dtype).cpu(), want)
 
 
-def test_no_numbers_stay_in_their_rows(gpu):
-    c = Case(200, 3, 96, 160, "even", whole=True)
+# (few rows, any alignment, 128 x 128 tiles in fp32 and large tiles in bf16)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("R,N,K", [(200, 300, 160), (24, 300, 320), (200, 301, 163), (3000, 6188, 528)])
+def test_no_numbers_stay_in_their_rows(gpu, R, N, K, dtype):
+    c = Case(R, 3, N, K, "even", whole=True)
     xq, xs = c.d[0], c.d[1]
-    xq[5, 7], xs[100, 1], xs[150, 0] = NAN_CODE, float("nan"), float("inf")
-    y = c.run(torch.float32)
+    xq[5, 7], xs[R // 2, 1], xs[R - 3, 0] = NAN_CODE, float("nan"), float("inf")
+    y = c.run(dtype)
     bad = (~torch.isfinite(y)).any(1).nonzero().reshape(-1).tolist()
-    assert bad == [5, 100, 150] and torch.isnan(y[[5, 100]]).all()
-    c = Case(200, 3, 300, 160, "even", whole=True)
-    c.d[4][1, 2, 0] = float("nan")  # columns 256.. of expert 1
-    y = torch.isnan(c.run(torch.float32))
-    a, b = int(c.offsets[1]), int(c.offsets[2])
-    assert y[a:b, 256:].all() and int(y.sum()) == (b - a) * 44
+    assert bad == [5, R // 2, R - 3] and torch.isnan(y[[5, R // 2]]).all()
+    c = Case(R, 3, N, K, "even", whole=True)
+    c.d[4][1, 2, 0] = float("nan")  # columns 256.. 383 of expert 1
+    y = torch.isnan(c.run(dtype))
+    a, b, end = int(c.offsets[1]), int(c.offsets[2]), min(N, 384)
+    assert y[a:b, 256:end].all() and int(y.sum()) == (b - a) * (end - 256)
 
 
 @pytest.mark.parametrize("shape", [(900, 4, 200, 2048, "ragged", 0), (1500, 3, 6208, 784, "even", 0),
