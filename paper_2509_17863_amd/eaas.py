@@ -490,23 +490,28 @@ def eaas_server_step(slots: torch.Tensor, n_slots: int, layers: torch.Tensor, n_
 # ------------------------------------------------------------ separate products
 def _rows(t: torch.Tensor, width: int, dtype=None) -> tuple[int, int]:
     """(pointer, elements between rows) of a 2-D tensor with dense rows."""
-    if t.dim() != 2 or t.shape[1] != width:
-        raise ValueError(f"expected rows of {width} elements, got {tuple(t.shape)}")
+    # (a small call is as long as its checks: each attribute is read once)
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != width:
+        raise ValueError(f"expected rows of {width} elements, got {tuple(shape)}")
     if dtype is not None and t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
         raise ValueError(f"expected {dtype}, got {t.dtype}")
-    if width > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if width > 1 and step != 1:
         raise ValueError("the elements of a row must be adjacent")
     # (one row, or none, may carry any stride)
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+    return t.data_ptr(), ld if shape[0] > 1 else width
 
 
 _OUT = {torch.bfloat16: EAAS_BF16, torch.float32: EAAS_FP32}
 
 
 def _dense(t: torch.Tensor, dtype, *shape) -> int:
-    if t.dtype != dtype or tuple(t.shape) != shape:
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-    return _p(t)
+    if not t.is_contiguous():
+        raise ValueError("tensor arguments must be contiguous")
+    return t.data_ptr()
 
 
 def _group_shape(R, E, N, K) -> _GroupShape:
