@@ -298,7 +298,11 @@ void grouped_fp8_kernel(GroupedParams p) {
 // The product on 128 x 128 tiles with codes converted to bf16 as fragments are read.  Four
 // waves, 64 x 64 results each, two LDS stages of both operands: a tile's loads are started
 // when every wave has read what the stage held, and waited for a tile later.  Two
-// workgroups to a CU cover each other's barriers, starts and stores.
+// workgroups to a CU cover each other's barriers, starts and stores.  8192^3: 0.98 ms, 1.12
+// PFLOP/s; 32768 rows of 32 experts, 7168 x 2048, fp32 results: 0.99 ms, 0.98.  Matrix pipes
+// are busy 48% of cycles and the vector units, 128 conversions a wave and tile among 250
+// instructions, the other half: the two hardly overlap (16 conversions beside two MFMAs take
+// 1.45 times those MFMAs' time).
 constexpr int kMidThreads = 256, kMidOperand = 16384, kMidStage = 2 * kMidOperand + 512;
 
 __global__ __launch_bounds__(kMidThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))

@@ -40,7 +40,11 @@
 // The products with an epilogue (grouped.h) run the same loop.  kSwiglu: a tile has 256 rows
 // of the result and 128 columns of h; its 256 rows of W are 32 gate rows, the up rows of the
 // same 32 columns, and so on, so that each wave of 64 holds both sums of 32 columns of h.
-// kSwigluGrad: a tile of dh as in kGradRows; gate and up are read on the way out.
+// kSwigluGrad: a tile of dh as in kGradRows; gate and up are read on the way out.  32768
+// rows of 32 experts, 4096 x 7168: 1.56 ms with the projections kept (the product alone 1.45
+// to 1.48, as is the gated one without them); 8192 rows of 8 experts, way back through 4096 x
+// 14336: 0.92 to 0.94 ms (dx alone 0.77): 0.12 to 0.17 of the way out is not hidden, since
+// all CUs reach it at the same time and it runs at memory's rate (1.2 GB).
 #pragma once
 
 #include <algorithm>
