@@ -279,7 +279,9 @@ EXACT = [(5, 1, 40, 70000, "one", 0), (20, 2, 96, 4096, "some", 4), (64, 1, 64, 
          (200, 2, 264, 9008, "one", 4), (9, 2, 33, 30001, "even", 3), (512, 16, 1024, 2048, "ragged", 2),
          (3000, 5, 6200, 528, "ragged", 0), (3000, 4, 6201, 1040, "some", 4),
          (2600, 5, 6144, 1300, "ragged", 0), (13, 1, 32, 448, "even", 0), (19, 1, 224, 6080, "even", 0),
-         (32, 1, 12256, 2192, "one", 4), (300, 7, 136, 64, "some", 3), (839, 1, 2048, 2592, "one", 0)]
+         (32, 1, 12256, 2192, "one", 4), (300, 7, 136, 64, "some", 3), (839, 1, 2048, 2592, "one", 0),
+         # large tiles whose sums are three and four blocks
+         (26638, 23, 416, 352, "even", 2), (1030, 63, 672, 512, "even", 0)]
 
 
 def test_every_kernel_is_among_these():
@@ -364,6 +366,35 @@ def test_offsets_that_do_not_ascend_stay_in_bounds(gpu, R, E, N, K):
     y = torch.empty((R, N), device="cuda")
     eaas.eaas_grouped_matmul_fp8(c.d[0], c.d[1], torch.from_numpy(off).cuda(), *c.d[3:], y, c.scratch)
     assert torch.equal(y, c.run(torch.float32))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(1500, 3, 6208, 784, "some", 0), (64, 8, 256, 272, "even", 2),
+                                   (300, 3, 136, 2000, "even", 0)], ids=str)
+def test_results_from_any_element(gpu, shape, dtype):
+    c = Case(*shape, whole=True)
+    want = torch.from_numpy(c.want()[0]).float().to(dtype)
+    for lead, pad in ((1, 0), (3, 5), (2, 1)):
+        flat = torch.full((lead + c.R * (c.N + pad) + 8,), CANARY, dtype=dtype, device="cuda")
+        y = flat[lead: lead + c.R * (c.N + pad)].view(c.R, c.N + pad)[:, : c.N]
+        eaas.eaas_grouped_matmul_fp8(*c.d, y, c.scratch, **c.take)
+        assert torch.equal(y[: c.live].cpu(), want)
+        y[: c.live] = CANARY
+        assert (flat == torch.tensor(CANARY, dtype=dtype)).all()
+
+
+def test_two_calls_at_once(gpu):
+    """On two streams, each with its workspace: large tiles beside a sum in parts."""
+    a, b = Case(1500, 3, 6208, 784, "even", whole=True), Case(20, 2, 96, 4096, "some", 4, whole=True)
+    want = [torch.from_numpy(c.want()[0]).float().to(torch.bfloat16) for c in (a, b)]
+    ys = [torch.empty((c.R, c.N), dtype=torch.bfloat16, device="cuda") for c in (a, b)]
+    streams = [torch.cuda.Stream() for _ in ys]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for c, y, s in zip((a, b), ys, streams):
+            eaas.eaas_grouped_matmul_fp8(*c.d, y, c.scratch, stream=s, **c.take)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y[: c.live].cpu(), w) for c, y, w in zip((a, b), ys, want))
 
 
 def test_gradient_in_the_rows_by_transposed_weights(gpu):

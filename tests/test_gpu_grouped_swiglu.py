@@ -202,7 +202,9 @@ WHOLE = [(5, 1, 40, 9000, "one", 0), (20, 2, 96, 1024, "some", 4), (64, 1, 64, 2
          (3000, 4, 3501, 264, "some", 4), (2600, 5, 3080, 392, "ragged", 0),
          (13, 1, 16, 2992, "even", 0), (263, 1, 160, 5232, "one", 0), (18, 1, 40, 176, "even", 3),
          (2981, 1, 496, 1808, "even", 0), (17, 1, 16, 3328, "even", 0), (362, 1, 272, 4320, "one", 0),
-         (2002, 1, 1632, 1760, "even", 0), (130, 3, 65, 65, "ragged", 0)]
+         (2002, 1, 1632, 1760, "even", 0), (130, 3, 65, 65, "ragged", 0),
+         # large tiles whose sums are three and four steps
+         (24506, 31, 240, 144, "even", 0), (28561, 14, 400, 160, "even", 0), (34026, 63, 16, 224, "even", 3)]
 
 
 def test_every_kernel_is_among_these():
@@ -325,6 +327,27 @@ def test_results_beside_one_another(gpu):
     h, gu = (torch.empty((R, n), dtype=torch.bfloat16, device="cuda") for n in (I, 2 * I))
     eaas.eaas_grouped_swiglu(x.cuda(), c.off, w.cuda(), h, ws, gu=gu)
     assert np.array_equal(v[:, :I], h[: c.live].double().cpu().numpy())
+
+
+@pytest.mark.parametrize("R,E,I,wide", [(1500, 3, 3104, 264), (1300, 4, 6200, 272), (64, 8, 128, 256),
+                                        (300, 2, 72, 2048)])
+def test_results_from_any_element(gpu, R, E, I, wide):
+    """Aligned operands (the kernels for those), results and projections from odd elements."""
+    for lead, pad in ((0, 0), (1, 3), (3, 0)):
+        c = Case(R, E, I, wide, "some")
+        x, w = c.make(R, wide), c.make(E, 2 * I, wide, scale=0.1)
+        h, gu = Place(R, I, lead, pad), Place(R, 2 * I, lead, pad)
+        eaas.eaas_grouped_swiglu(x.cuda(), c.off, w.cuda(), h.t,
+                                 eaas.alloc_grouped_workspace(R, E, 2 * I, wide), gu=gu.t)
+        check_forward(c, h, gu, L.grouped_swiglu(x.double().numpy(), c.offsets, w.double().numpy(), np.arange(R)))
+        dy, wd = c.make(R, wide), c.make(E, wide, I, scale=0.1)
+        proj = rounded(c.rng.normal(size=(R, 2 * I)))
+        gud, dgu, h = Place(R, 2 * I, lead, pad, proj), Place(R, 2 * I, lead, pad), Place(R, I, lead, pad)
+        eaas.eaas_grouped_swiglu_backward(dy.cuda(), c.off, wd.cuda(), gud.t, dgu.t,
+                                          eaas.alloc_grouped_workspace(R, E, wide, I), h=h.t)
+        a = proj[: c.live].double().numpy()
+        check_backward(c, dgu, h, a, L.grouped_swiglu_backward(dy.double().numpy(), c.offsets,
+                                                               wd.double().numpy(), a))
 
 
 def test_rows_past_32_bit_offsets(gpu):
