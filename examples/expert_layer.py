@@ -108,11 +108,13 @@ class FusedExpertLayer(ExpertLayer):
 
 class Fp8Experts:
     """The experts in e4m3: weights with a scale for each block of 128 x 128, quantized
-    once; activations with a scale for each 128 columns of a row, quantized on the way."""
+    once; activations with a scale for each 128 columns of a row, quantized on the way.
+    short_sums: the bf16 sums of gate and up may keep less than fp32 (about half the time of
+    a large batch's product)."""
 
-    def __init__(self, T, k, w_gate_up, w_down):
+    def __init__(self, T, k, w_gate_up, w_down, short_sums=False):
         self.E, two_i, self.H = w_gate_up.shape
-        self.T, self.k, self.I = T, k, two_i // 2
+        self.T, self.k, self.I, self.short_sums = T, k, two_i // 2, short_sums
         R, hb, ib = T * k, (self.H + 127) // 128, (self.I + 127) // 128
         self.gate_up_q, self.gate_up_s = self._weights(w_gate_up)
         self.down_q, self.down_s = self._weights(w_down)
@@ -141,7 +143,8 @@ class Fp8Experts:
         off = r["offsets"]
         eaas.eaas_quantize_blocks_fp8(x, self.xq, self.xs)
         eaas.eaas_grouped_matmul_fp8(self.xq, self.xs, off, self.gate_up_q, self.gate_up_s,
-                                     self.gate_up, self.ws, perm=r["perm"], k=self.k)
+                                     self.gate_up, self.ws, perm=r["perm"], k=self.k,
+                                     short_sums=self.short_sums)
         eaas.eaas_swiglu_fp8(self.gate_up, self.hq, self.hs, n_rows=off[self.E:])
         eaas.eaas_grouped_matmul_fp8(self.hq, self.hs, off, self.down_q, self.down_s, self.y,
                                      self.ws)

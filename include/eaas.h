@@ -96,7 +96,10 @@ enum eaas_dtype {
    * eaas_tile_weights_fp8 writes, which the decode-sized fp8 GEMMs stream as
    * contiguous blocks instead of rows K bytes apart.  Needs H a multiple of
    * 256.  Accepted by every entry point that takes a weight dtype. */
-  EAAS_FP8_E4M3_TILED = 4
+  EAAS_FP8_E4M3_TILED = 4,
+  /* As the type of eaas_grouped_matmul_fp8's results: bf16, and sums in fewer bits than
+   * fp32 where that is faster (see there). */
+  EAAS_BF16_SHORT_SUMS = 5
 };
 
 /*
@@ -518,12 +521,13 @@ size_t eaas_grouped_fp8_workspace_bytes(const eaas_group_shape *s);
  * over the blocks b of 128 columns (the last one may be narrower).
  *   xq [R or R/k, K] contiguous with xs [.., ceil(K/128)] fp32; wq [E,N,K], 16-byte
  *   aligned, with wscale [E,ceil(N/128),ceil(K/128)] fp32; y [R,N] bf16 or fp32 (ldy)
- * fp32 results: products are exact and every sum is taken in fp32.  bf16 results of
- * large groups come from the 8-bit floating matrix instructions: eight products at a
- * time are added after each has been rounded to a multiple of 2^-13 of the power of two
- * under the largest of them, which moves a result by at most 7 * 2^-14 of its terms'
- * magnitudes in all (by 2^-16 of the results' norm for normal data; the rounding to bf16
- * is 2^-8).  The sums of the blocks are added in fp32 either way.
+ * Products are exact and every sum is taken in fp32.  With y_dtype EAAS_BF16_SHORT_SUMS the
+ * bf16 results of large groups come from the 8-bit floating matrix instructions, at up to
+ * twice the rate: eight products at a time are added after each has been rounded to a
+ * multiple of 2^-13 of the power of two under the largest of them, which moves a result by
+ * at most 7 * 2^-14 of its terms' magnitudes in all (by 2^-16 of the results' norm for
+ * normal data; the rounding to bf16 is 2^-8).  Whether a group is large depends on the
+ * batch, and so do such results.  The sums of the blocks are added in fp32 either way.
  * Gradient in the rows: the same call with the transposed codes [E,K,N] and scales
  * [E,ceil(K/128),ceil(N/128)], and dy quantized as rows.
  * ws of eaas_grouped_fp8_workspace_bytes.  Errors as eaas_grouped_matmul. */

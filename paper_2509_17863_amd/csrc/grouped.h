@@ -344,7 +344,7 @@ hipError_t launch_grouped_swiglu_pp(const GroupedParams& p, long long tiles, hip
 hipError_t launch_grouped_swiglu_grad_pp(const GroupedParams& p, long long tiles,
                                          hipStream_t stream);
 
-// grouped_fp8.hip: the same for block-scaled e4m3, bf16 results.
+// grouped_fp8.hip: the same for block-scaled e4m3, bf16 results, short sums.
 hipError_t launch_grouped_fp8_pp(const GroupedParams& p, long long tiles, hipStream_t stream);
 
 // The same operands on 128 x 128 tiles, fp32 sums of exact products.

@@ -497,7 +497,8 @@ GroupedPlan grouped_plan(const GroupedArgs& a, bool in16) {
   any.splits = best_parts(steps, out, [&](int s) { return any_us(tiles, steps, s); }, &t_any);
   if (!in16) return any;
   if (a.dir == kGradWeights) return rows >= 128 && large >= 48 ? on_large : any;
-  const bool has_large = a.type != kFp8 || !a.out_fp32;
+  // (large tiles of e4m3: the matrix instructions' own sums, grouped_fp8.hip)
+  const bool has_large = a.type != kFp8 || a.short_sums;
   const int some = a.dir == kForward && a.type == kBf16 ? 48 : 16;
   if (has_large && rows >= some && large >= 192 && steps >= 4) return on_large;
   GroupedPlan few{kFew, rows <= 12 ? 16 : rows <= 24 ? 32 : 64, 64, 1};

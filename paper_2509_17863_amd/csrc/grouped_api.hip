@@ -87,7 +87,8 @@ int forward(const eaas_group_shape* s, const void* x, long long ldx, const float
             const int32_t* perm, int32_t k, const int32_t* offsets, const void* w,
             const float* wscale, void* y, long long ldy, int y_dtype, int type, void* ws,
             size_t ws_bytes, void* stream) {
-  const bool scaled = type != kBf16;
+  const bool scaled = type != kBf16, short_sums = type == kFp8 && y_dtype == EAAS_BF16_SHORT_SUMS;
+  if (short_sums) y_dtype = EAAS_BF16;
   const int esz = scaled ? 1 : 2, osz = y_dtype == EAAS_FP32 ? 4 : 2;
   int st = check_group(s);
   if (st != EAAS_OK) return st;
@@ -120,6 +121,7 @@ int forward(const eaas_group_shape* s, const void* x, long long ldx, const float
   a.out = y;
   a.ldo = ldy;
   a.out_fp32 = y_dtype == EAAS_FP32;
+  a.short_sums = short_sums;
   a.row_scale = xs;
   a.col_scale = wscale;
   return enqueue(a, ws, ws_bytes, stream);
@@ -150,8 +152,8 @@ size_t eaas_grouped_fp8_workspace_bytes(const eaas_group_shape* s) {
   if (check_group(s) != EAAS_OK) return 0;
   size_t n = 256;
   GroupedArgs a = args_of(s, kForward, kFp8);
-  for (const bool fp32 : {false, true}) {
-    a.out_fp32 = fp32;
+  for (const bool short_sums : {false, true}) {
+    a.short_sums = short_sums;
     n = std::max(n, grouped_workspace_most(a));
   }
   return (n + 255) / 256 * 256;
@@ -445,9 +447,9 @@ int eaas_unpermute_combine_backward(const eaas_shape* s, const void* dout, int d
 
 // Not part of the ABI: the kernel that a product takes, for tests and measurements
 // (grouped_plan_code), or -1 for what the library rejects.  dir: 0 forward, 1 gradient
-// in the rows, 2 in the weights; type: 0 bf16, 1 8-bit integers, 2 e4m3 with bf16 results
+// in the rows, 2 in the weights; type: 0 bf16, 1 8-bit integers, 2 e4m3 with short sums
 // (forward); 3 the product in dir with its epilogue (kSwiglu, kSwigluGrad); 4 e4m3 with
-// fp32 results; in16: sizes, strides and bases in multiples of 16 bytes.
+// sums in fp32; in16: sizes, strides and bases in multiples of 16 bytes.
 int eaas_internal_grouped_plan(const eaas_group_shape* s, int dir, int type, int in16) {
   if (check_group(s) != EAAS_OK || dir < kForward || dir > kGradWeights || type < 0 || type > 4)
     return -1;
@@ -458,7 +460,7 @@ int eaas_internal_grouped_plan(const eaas_group_shape* s, int dir, int type, int
   }
   if (type != kBf16 && dir != kForward) return -1;
   GroupedArgs a = args_of(s, dir, type == 4 ? kFp8 : type);
-  a.out_fp32 = type == 4;
+  a.short_sums = type == 2;
   return grouped_plan_code(a, in16 != 0);
 }
 

@@ -176,6 +176,7 @@ struct GroupedArgs {
   void* out;
   long long ldo;
   bool out_fp32, accumulate;
+  bool short_sums;          // kFp8: sums of fewer bits than fp32 will do
   const float* row_scale;   // 8-bit operands
   const float* col_scale;
   // kSwiglu: out is h, gu (or nullptr) gets the sums; kSwigluGrad: out is dgu, gu is read,

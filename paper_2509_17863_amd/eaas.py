@@ -35,6 +35,7 @@ __all__ = [
 
 EAAS_OK = 0
 EAAS_BF16, EAAS_FP8_E4M3, EAAS_FP32, EAAS_FP8_E4M3_A8, EAAS_FP8_E4M3_TILED = 0, 1, 2, 3, 4
+EAAS_BF16_SHORT_SUMS = 5
 EAAS_GATE_UP, EAAS_DOWN = 0, 1
 EAAS_SLOT_EMPTY, EAAS_SLOT_READY, EAAS_SLOT_DONE, EAAS_SLOT_OFFLINE = 0, 1, 2, 3
 EAAS_WS_H, EAAS_WS_HQ, EAAS_WS_HS, EAAS_WS_XQ, EAAS_WS_XS, EAAS_WS_STAGE = range(6)
@@ -535,12 +536,12 @@ _GROUPED_KERNELS = ("any", "few", "large")
 
 def _grouped_plan(product: str, R, E, N, K, in16: bool) -> tuple[str, int, int]:
     """(kernel, rows of its tiles, parts of the sum) of the product "forward", "dx",
-    "dw", "int8", "fp8" (bf16 results), "fp8_fp32", "swiglu" or "swiglu_backward": the
-    library's own choice, asked on the host, for tests and measurements.  in16: sizes,
-    strides and bases are multiples of 16 bytes."""
+    "dw", "int8", "fp8" (short sums), "fp8_fp32" (sums in fp32), "swiglu" or
+    "swiglu_backward": the library's own choice, asked on the host, for tests and
+    measurements.  in16: sizes, strides and bases are multiples of 16 bytes."""
     s = _group_shape(R, E, N, K)
-    d, kind = {"forward": (0, 0), "dx": (1, 0), "dw": (2, 0), "int8": (0, 1), "fp8": (0, 2), "fp8_fp32": (0, 4),
-               "swiglu": (0, 3), "swiglu_backward": (1, 3)}[product]
+    d, kind = {"forward": (0, 0), "dx": (1, 0), "dw": (2, 0), "int8": (0, 1), "fp8": (0, 2),
+               "fp8_fp32": (0, 4), "swiglu": (0, 3), "swiglu_backward": (1, 3)}[product]
     r = int(lib().eaas_internal_grouped_plan(ctypes.byref(s), d, kind, int(in16)))
     if r < 0:
         raise EaasError(-2, "eaas_internal_grouped_plan")
@@ -692,22 +693,26 @@ def alloc_grouped_fp8_workspace(R, E, N, K, device="cuda") -> torch.Tensor:
 
 def eaas_grouped_matmul_fp8(xq: torch.Tensor, xs: torch.Tensor, offsets: torch.Tensor,
                             wq: torch.Tensor, wscale: torch.Tensor, y: torch.Tensor,
-                            ws: torch.Tensor, perm=None, k: int = 1, stream=None) -> None:
+                            ws: torch.Tensor, perm=None, k: int = 1, stream=None,
+                            short_sums: bool = False) -> None:
     """The product of e4m3 codes with scales for each block of 128
     (eaas_quantize_blocks_fp8): xq [R, K] (or the tokens, with perm) with xs [.., K/128],
     wq [E, N, K] with wscale [E, N/128, K/128] (quotients rounded up), y [R, N] bf16 or
-    fp32."""
+    fp32.  Sums are fp32; short_sums allows the 8-bit matrix instructions' for large groups
+    with bf16 results, which keep 13 bits below the largest of eight products (EAAS_BF16_SHORT_SUMS
+    in eaas.h) and take about half the time."""
     E, N, K = wq.shape
     R = y.shape[0]
-    yp, ldy = _rows(y, N, (torch.bfloat16, torch.float32))
+    yp, ldy = _rows(y, N, torch.bfloat16 if short_sums else (torch.bfloat16, torch.float32))
     pp, kk = _gather(xq, R, perm, k)
     s = _group_shape(R, E, N, K)
     _check(lib().eaas_grouped_matmul_fp8(
         ctypes.byref(s), _codes(xq, xq.shape[0], K),
         _dense(xs, torch.float32, xq.shape[0], _blocks(K)), pp, kk,
         _dense(offsets, torch.int32, E + 1), _codes(wq, E, N, K),
-        _dense(wscale, torch.float32, E, _blocks(N), _blocks(K)), yp, ldy, _OUT[y.dtype], _p(ws),
-        ws.numel(), _stream(stream)), "eaas_grouped_matmul_fp8")
+        _dense(wscale, torch.float32, E, _blocks(N), _blocks(K)), yp, ldy,
+        EAAS_BF16_SHORT_SUMS if short_sums else _OUT[y.dtype], _p(ws), ws.numel(),
+        _stream(stream)), "eaas_grouped_matmul_fp8")
 
 
 def eaas_grouped_swiglu(x: torch.Tensor, offsets: torch.Tensor, w: torch.Tensor, h: torch.Tensor,
