@@ -527,7 +527,9 @@ size_t eaas_grouped_fp8_workspace_bytes(const eaas_group_shape *s);
  * multiple of 2^-13 of the power of two under the largest of them, which moves a result by
  * at most 7 * 2^-14 of its terms' magnitudes in all (by 2^-16 of the results' norm for
  * normal data; the rounding to bf16 is 2^-8).  Whether a group is large depends on the
- * batch, and so do such results.  The sums of the blocks are added in fp32 either way.
+ * batch, and so do such results.  Products of a row's scale and a block's have to lie in
+ * fp32's normal range (or be zero) there; otherwise results alone have to lie in fp32's.  The
+ * sums of the blocks are added in fp32 either way.
  * Gradient in the rows: the same call with the transposed codes [E,K,N] and scales
  * [E,ceil(K/128),ceil(N/128)], and dy quantized as rows.
  * ws of eaas_grouped_fp8_workspace_bytes.  Errors as eaas_grouped_matmul. */

@@ -257,13 +257,26 @@ void grouped_any_kernel(GroupedParams p) {
       if constexpr (FP8) {
         f32x16 part[2][2];
         fp8_block(sa, wi, sb, wj, part);
+        float rs[2];
+        const float cs = col_scale[kt];
+        bool far = false;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float f = row_scale[i][kt] * col_scale[kt];
+          rs[i] = row_scale[i][kt];
+          const float f = scale_of(rs[i], cs, far);
 #pragma unroll
           for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = fmaf(part[i][j][v], f, acc[i][j][v]);
+        }
+        if (__builtin_expect(__any(far), false)) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+              for (int v = 0; v < 16; ++v)
+                acc[i][j][v] = add_far(part[i][j][v], rs[i], cs, acc[i][j][v]);
         }
         __syncthreads();
         continue;

@@ -158,7 +158,8 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[i][j] = Acc{};
   const LDS_AS char* ring = (const LDS_AS char*)smem_raw + wave * STAGES * kStage;
-  auto multiply = [&](const LDS_AS char* stage, float col) {
+  // (cs: the columns' scale, row: the rows' where a register has it)
+  auto multiply = [&](const LDS_AS char* stage, float row, float cs) {
     f32x4 part[FP8 ? MB : 1][FP8 ? NB : 1];
     if constexpr (FP8) {
 #pragma unroll
@@ -226,15 +227,26 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
         }
     }
     if constexpr (FP8) {
+      float rs[MB];
+      bool far = false;
 #pragma unroll
       for (int i = 0; i < MB; ++i) {
-        float f = col;
-        if constexpr (S_STAGE)
-          f *= *reinterpret_cast<const LDS_AS float*>(stage + kWBytes + kXBytes + (i * 16 + l16) * 4);
+        rs[i] = S_REG ? row : *reinterpret_cast<const LDS_AS float*>(stage + kWBytes + kXBytes +
+                                                                     (i * 16 + l16) * 4);
+        const float f = scale_of(rs[i], cs, far);
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
           for (int v = 0; v < 4; ++v) acc[i][j][v] = fmaf(part[i][j][v], f, acc[i][j][v]);
+      }
+      if (__builtin_expect(__any(far), false)) {
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+              acc[i][j][v] = add_far(part[i][j][v], rs[i], cs, acc[i][j][v]);
       }
     }
   };
@@ -257,8 +269,8 @@ __global__ __launch_bounds__(kThreads) void grouped_few_kernel(GroupedParams p) 
     if (kt + STAGES <= nk) wait_vmcnt<(STAGES - 1) * INST>();
     else wait_vmcnt<0>();
     asm volatile("" ::: "memory");
-    multiply(ring + (kt % STAGES) * kStage,
-             S_REG ? col * __shfl(four, (kt & 3) * 16 + l16, kWave) : col);
+    multiply(ring + (kt % STAGES) * kStage, S_REG ? __shfl(four, (kt & 3) * 16 + l16, kWave) : 0.0f,
+             col);
     col = next;
     // the stage is read: it may be filled again
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");

@@ -168,7 +168,9 @@ void grouped_fp8_kernel(GroupedParams p) {
   f32x4 acc[8][4];
   struct Frags {
     i32x8 a[8], b[4];
-    float f[8];  // scale of the block's rows times the columns'
+    // scale of the block's rows times the columns' (in range, by the call's contract: a second
+    // way to add them here spills 300 registers and more)
+    float f[8];
   };
   const CONST_AS float* col_scale = nullptr;
   auto fragment = [&](const LDS_AS char* block, int at) INLINE {
@@ -376,16 +378,28 @@ void grouped_fp8_mid_kernel(GroupedParams p) {
     const float col = col_scale[kt];
     f32x16 part[2][2];
     fp8_block(stage, wi, stage + kMidOperand, wj, part);
+    float row[2];
+    bool far = false;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const float f = *reinterpret_cast<const LDS_AS float*>(stage + 2 * kMidOperand +
-                                                             (wi + 32 * i + (lane & 31)) * 4) * col;
+      row[i] = *reinterpret_cast<const LDS_AS float*>(stage + 2 * kMidOperand +
+                                                      (wi + 32 * i + (lane & 31)) * 4);
+      const float f = scale_of(row[i], col, far);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[i][j][v] = fmaf(part[i][j][v], f, acc[i][j][v]);
         asm volatile("" : "+v"(acc[i][j]));  // (not behind the next barrier)
       }
+    }
+    if (__builtin_expect(__any(far), false)) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            acc[i][j][v] = add_far(part[i][j][v], row[i], col, acc[i][j][v]);
     }
   }
   __syncthreads();
