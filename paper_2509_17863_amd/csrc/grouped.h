@@ -248,7 +248,7 @@ __device__ __forceinline__ void store_swiglu(const GroupedParams& p, size_t i, i
                                              const float (&g)[8], const float (&u)[8]) {
   float h[8];
 #pragma unroll
-  for (int c = 0; c < 8; ++c) h[c] = silu_up(g[c], u[c]);
+  for (int c = 0; c < 8; ++c) h[c] = gated(g[c], u[c]);
   store8(static_cast<uint16_t*>(p.out) + i * p.ldo + j, n, h);
   if (p.gu) {
     uint16_t* at = p.gu + i * p.ldgu + j;
@@ -305,7 +305,7 @@ __device__ __forceinline__ void store_swiglu_grad(const GroupedParams& p, size_t
     const SwigluGrad t0 = swiglu_grad(g0, u0, dh[2 * c]), t1 = swiglu_grad(g1, u1, dh[2 * c + 1]);
     dg[c] = to_bf16x2(t0.gate, t1.gate);
     du[c] = to_bf16x2(t0.up, t1.up);
-    h[c] = to_bf16x2(silu_up(g0, u0), silu_up(g1, u1));
+    h[c] = to_bf16x2(gated(g0, u0), gated(g1, u1));
   }
   uint16_t* to = static_cast<uint16_t*>(p.out) + i * p.ldo + j;
   store8_raw(to, n, dg, far);
@@ -319,7 +319,7 @@ __device__ __forceinline__ void store_one(const GroupedParams& p, size_t i, int 
   uint16_t* to = static_cast<uint16_t*>(p.out) + i * p.ldo + j;
   auto bits = [](float v) { return (uint16_t)to_bf16x2(v, 0.0f); };
   if constexpr (EPI == kSwiglu) {
-    *to = bits(silu_up(a, b));
+    *to = bits(gated(a, b));
     if (p.gu) {
       p.gu[i * p.ldgu + j] = bits(a);
       p.gu[i * p.ldgu + j + p.N / 2] = bits(b);
@@ -331,7 +331,7 @@ __device__ __forceinline__ void store_one(const GroupedParams& p, size_t i, int 
     const SwigluGrad t = swiglu_grad(g, u, a);
     to[0] = bits(t.gate);
     to[p.K] = bits(t.up);
-    if (p.h) p.h[i * p.ldh + j] = bits(silu_up(g, u));
+    if (p.h) p.h[i * p.ldh + j] = bits(gated(g, u));
   }
 }
 

@@ -300,7 +300,7 @@ __device__ __forceinline__ void store_swiglu_results(const GroupedParams& p, con
     for (int q = 0; q < 4; ++q) {
       float v[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) v[c] = silu_up(acc[i][0][4 * q + c], acc[i][1][4 * q + c]);
+      for (int c = 0; c < 4; ++c) v[c] = gated(acc[i][0][4 * q + c], acc[i][1][4 * q + c]);
       *reinterpret_cast<LDS_AS u32x2*>(buf + lrow * 64 + ((q ^ ((lrow >> 1) & 3)) << 4) + khalf * 8) =
           u32x2{to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3])};
     }
