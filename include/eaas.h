@@ -508,8 +508,9 @@ int eaas_grouped_matmul_int8(const eaas_group_shape *s, const void *xq, const fl
  * e4m3fn(x/s) to the nearest, ties to even, saturated at +-448; product and quotients in
  * fp32, correctly rounded.  (eaas_quantize_rows_fp8 divides by 448: its scales differ by a
  * unit in the last place at most.)  A block that holds an infinity or a NaN gets a NaN
- * scale and zero codes, so whatever is computed from it is NaN.  rows or mats = 0: nothing.  Errors: INVALID_ARG (also overlaps), UNSUPPORTED
- * (mats*rows above 2^31 - 1, K or ldx above 2^22), HIP. */
+ * scale and zero codes, so whatever is computed from it is NaN.  rows or mats = 0:
+ * nothing.  Errors: INVALID_ARG (also overlaps), UNSUPPORTED (mats*rows above 2^31 - 1, K
+ * or ldx above 2^22), HIP. */
 int eaas_quantize_blocks_fp8(const void *x, int x_dtype, int64_t ldx, int32_t mats, int64_t rows,
                              int32_t K, int32_t block_rows, void *q, float *s, void *stream);
 

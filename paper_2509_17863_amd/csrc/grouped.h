@@ -1,5 +1,5 @@
-// Device-side parts shared by the grouped product kernels (grouped.hip and
-// grouped_fast.hip): parameters, the tile a workgroup works on, and stores.
+// Device-side parts shared by the grouped product kernels (grouped.hip, grouped_few.hip,
+// grouped_pp.h and grouped_fp8.hip): parameters, the tile a workgroup works on, and stores.
 //
 // One frame holds the three products of an expert's matrix W [N,K]:
 //   kForward   y[r,n]   = sum_k x[r,k] W[n,k]     i = r, j = n, sum over k
@@ -335,7 +335,8 @@ __device__ __forceinline__ void store_one(const GroupedParams& p, size_t i, int 
   }
 }
 
-// grouped_fast.hip: 256 x 256 tiles, sizes and addresses in multiples of 16 bytes.
+// grouped_pp.h (compiled in grouped_fast.hip): 256 x 256 tiles, sizes and addresses in
+// multiples of 16 bytes.
 template <int DIR, bool I8>
 hipError_t launch_grouped_pp(const GroupedParams& p, long long tiles, hipStream_t stream);
 

@@ -17,9 +17,9 @@
 // What bounds it: loads that straddle lines (a wave's 16-byte loads take 7.6 ns on
 // aligned rows, 13.8 where rows start on any dword, 27 on any 2 bytes), then LDS.
 // 8 experts of 1024 rows, 4097 x 8191: forward 0.90 ms (608 TFLOP/s), dx 0.96, dW
-// 0.94; 8-bit integers 0.54 (1025 TOP/s).  e4m3 takes 244 registers, so two workgroups to a
+// 0.94; 8-bit integers 0.54 (1025 TOP/s).  e4m3 takes 252 registers, so two workgroups to a
 // CU, and is bound by its conversions beside the MFMAs (grouped_fp8.hip): 4662 rows of 24
-// experts, 1283 x 1921, 82 us, where 1.03 rounds of workgroups take two.
+// experts, 1283 x 1921, 87 us, where 1.03 rounds of workgroups take two.
 #include <algorithm>
 
 #include "grouped_fast.h"

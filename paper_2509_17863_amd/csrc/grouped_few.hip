@@ -14,14 +14,14 @@
 //
 // kSwiglu: the 64 weight rows are 32 gate rows and the up rows of the same columns.  kFp8:
 // a tile of the sum is one block of scales; the rows' scales travel in the stage, and codes
-// go to bf16 as they are read (grouped.hip, fp8_block), which memory leaves time for.
+// go to bf16 as they are read (as in grouped_fast.h, fp8_block), which memory leaves time for.
 //
-// Measured, reading the weights once: e4m3, 8 tokens on 128 experts, 1536 x 2048: 29 us (5.1
-// TB/s), one token on 8 experts, 4096 x 7168: 37 (6.3); gated, 32 rows of 8 experts, 28672 x
-// 4096: 300 (6.3), its way back, 4 rows of each of 128 experts, 2048 x 768: 73 (5.5); 4 rows of each of 128 experts, 2048 x 768:
-// forward 76 us (5.3 TB/s), dx 71 (5.6); one token, 8 of 32
-// experts, 4096 x 7168 in 8-bit integers: 37 us (6.4); 8 tokens on 128 experts, 1536 x
-// 2048: 50 (6.3).
+// Measured, reading the weights once:
+//   bf16, 4 rows of each of 128 experts, 2048 x 768: forward 76 us (5.3 TB/s), dx 71 (5.6),
+//   the gated product's way back 73 (5.5); gated, 32 rows of 8 experts, 28672 x 4096: 300 (6.3)
+//   8-bit integers, one token on 8 experts, 4096 x 7168: 37 us (6.4); 8 tokens on 128 experts,
+//   1536 x 2048: 50 (6.3)
+//   e4m3, the same two: 37 to 39 us (6.0 to 6.3), 29 to 30 (5.0)
 #include "grouped_fast.h"
 
 namespace eaas {

@@ -23,8 +23,9 @@
 // t had is free, so no third one is needed, and the scales and the way out have room.  A
 // row's scales for four tiles are one load of 16 bytes where rows of scales allow it.
 //
-// 32768 rows of 32 experts, 4096 x 7168: 0.89 ms, 2.17 PFLOP/s; 8192^3: 0.49 ms, 2.25 (the
-// loads of B ahead of C's first instruction: 0.92; and scales one at a time: 1.07).  Without
+// 32 equal groups of 1024 rows, 4096 x 7168: 0.89 ms, 2.16 PFLOP/s (unevenly used experts:
+// 0.98); 8192^3: 0.48 ms, 2.29 (the loads of B ahead of C's first instruction: 0.92 on the
+// equal groups; and scales one at a time: 1.07).  Without
 // loads the loop takes 0.64: what bounds it is their latency, which two stages cover by two
 // phases.  Five half stages of B with all loads in M phases, half of them a phase earlier,
 // took 0.87, but 0.52 ms instead of 0.49 where K is 2048.
@@ -302,9 +303,10 @@ void grouped_fp8_kernel(GroupedParams p) {
 // The product on 128 x 128 tiles with codes converted to bf16 as fragments are read.  Four
 // waves, 64 x 64 results each, two LDS stages of both operands: a tile's loads are started
 // when every wave has read what the stage held, and waited for a tile later.  Two
-// workgroups to a CU cover each other's barriers, starts and stores.  8192^3: 0.98 ms, 1.12
-// PFLOP/s; 32768 rows of 32 experts, 7168 x 2048, fp32 results: 0.99 ms, 0.98.  Matrix pipes
-// are busy 48% of cycles and the vector units, 128 conversions a wave and tile among 250
+// workgroups to a CU cover each other's barriers, starts and stores.  8192^3: 0.97 ms, 1.13
+// PFLOP/s (fp32 results: 0.99, 1.11); 32 equal groups of 1024 rows, 4096 x 7168: 1.79 ms, 1.08;
+// 7168 x 2048, fp32 results: 1.01 ms, 0.95 (unevenly used experts: 1.98 and 1.14).  Matrix pipes
+// are busy 47 to 54% of cycles and the vector units, 128 conversions a wave and tile among 250
 // instructions, the other half: the two hardly overlap (16 conversions beside two MFMAs take
 // 1.45 times those MFMAs' time).
 constexpr int kMidThreads = 256, kMidOperand = 16384, kMidStage = 2 * kMidOperand + 512;
